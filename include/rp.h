@@ -238,6 +238,112 @@ rp_status rp_lse_combine(const float* o_parts, const float* lse_parts,
                          const int32_t* row_part_offsets, int32_t num_rows, int32_t head_dim,
                          void* out, float* lse_out, hipStream_t stream);
 
+/* ---- Trees of drafted tokens ------------------------------------------
+ * Speculative decoding drafts several tokens per sequence and verifies them in
+ * one step: sequence s has n_s = draft_offs[s+1] - draft_offs[s] drafted
+ * tokens, packed in rows draft_offs[s] .. draft_offs[s+1]-1 of the arrays
+ * below. Draft i of s attends to the keys that rp_group_decode_attn reads for
+ * s (its group's prefix, its resp_lens[s] response tokens), and to the drafts
+ * u < n_s of s whose bit u is set in masks[draft_offs[s] + i]: in a tree its
+ * ancestors and itself. Any other mask is as good: bits at or above n_s are
+ * ignored, and a draft that sees no key has out = 0 and lse = -inf. Drafts
+ * that a row does not see do not enter its result whatever they hold
+ * (infinities and NaN included). */
+typedef struct {
+  int32_t num_drafts;         /* T, rows of the packed arrays (draft_offs[S], or more) */
+  int32_t max_drafts;         /* no n_s is larger; 1 .. 64 */
+  const int32_t* draft_offs;  /* [S + 1], non-decreasing, draft_offs[0] = 0, draft_offs[S] <= T */
+  const uint64_t* masks;      /* [T] */
+} rp_draft_tree;
+
+/* Workspace bytes needed by rp_group_tree_attn for this shape (0 for small
+ * ones). Depends only on host-side scalars; *bytes is a host pointer. */
+rp_status rp_group_tree_attn_workspace_size(const rp_paged_kv* kv, const rp_group_layout* layout,
+                                            const rp_draft_tree* tree, size_t* bytes);
+
+/* Attention of every drafted token (paper, Section 4: a decode step of the
+ * rollout node's workers, here over several tokens per sequence; each group's
+ * prefix is still read once for all of its members, Section 2.1).
+ * q: bf16 [T][Hq][head_dim]; k_draft, v_draft: bf16 [T][Hkv][head_dim], the
+ * drafts' own keys and values, which are not in the cache (also for fp8
+ * pools): accepted ones are written there afterwards (rp_kv_write_slots).
+ * out: bf16 [T][Hq][head_dim]; all 16-byte aligned. lse: fp32 [T][Hq], natural
+ * log, may be NULL. Rows from draft_offs[S] on are neither read nor written.
+ * softmax_scale must be finite and > 0. Probabilities are rounded to bf16 for
+ * their product with V; sums, maxima and outputs are held in fp32.
+ * workspace: device buffer of at least rp_group_tree_attn_workspace_size
+ * bytes, 256-byte aligned (may be NULL when that is 0); concurrent calls need
+ * distinct workspaces. */
+rp_status rp_group_tree_attn(const rp_paged_kv* kv, const rp_group_layout* layout, const rp_draft_tree* tree,
+                             const void* q, const void* k_draft, const void* v_draft, float softmax_scale,
+                             void* out, float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ---- Page tables and writes by slot ---------------------------------------
+ * The tables that a layout points at, kept on the device: sequences (or
+ * groups' prefixes) take pages from a stack of free page ids as they grow and
+ * give them back as they shrink or end, without a copy to the host.
+ *
+ * A slot is page * 16 + row: the place of one token in every (page, kv-head)
+ * block of a pool. */
+typedef struct {
+  int32_t num_seqs;       /* S <= 4096, rows of the table */
+  int32_t max_pages;      /* width of the table */
+  int32_t page_size;      /* 16 */
+  int32_t num_pages;      /* pages of the pool, and entries of free_pages */
+  int32_t* block_table;   /* [S][max_pages], in and out */
+  int32_t* free_pages;    /* [num_pages], the first free_count[0] of them a stack; in and out */
+  int32_t* free_count;    /* [1], in and out */
+} rp_page_tables;
+
+/* status[0] of rp_page_tables_resize, on the device. */
+typedef enum {
+  RP_TABLES_OK = 0,
+  RP_TABLES_NO_PAGES = 1,       /* fewer free pages than the call takes */
+  RP_TABLES_BAD_LENGTH = 2,     /* a length below 0 or above max_pages * 16 */
+  RP_TABLES_NO_SLOTS = 3,       /* more new tokens than max_slots (or than an int32 counts) */
+  RP_TABLES_BAD_FREE_LIST = 4   /* free_count below 0, or above num_pages with the pages given back */
+} rp_tables_status;
+
+/* Sequence s goes from old_lens[s] to new_lens[s] tokens (int32 [S], which the
+ * call only reads; [1024, 0] ends a sequence, equal lengths leave it). With
+ * pages(x) = ceil(x / 16), F = sum max(pages(old) - pages(new), 0) pages are
+ * given back and N = sum max(pages(new) - pages(old), 0) taken. The page given
+ * back with rank f, counted by sequence and then by place in the table, goes to
+ * free_pages[C + F - 1 - f], C being free_count; then the page of rank o,
+ * counted the same way, is taken from free_pages[C + F - 1 - o]; free_count
+ * becomes C + F - N. Table entries given back become -1, others are left. So a
+ * call followed by its opposite leaves tables and stack as they were, and pages
+ * given back are taken first.
+ * slot_offs (int32 [S + 1], or NULL): exclusive sums of the new tokens
+ * max(new - old, 0), the total last. slot_map (int32 [max_slots], or NULL; needs
+ * slot_offs): the slots of every sequence's tokens old .. new - 1, packed by
+ * sequence, then -1 up to max_slots: what rp_kv_write_slots takes.
+ * All or nothing: status (int32 [4], device) gets {rp_tables_status, N, F, new
+ * tokens}; unless status[0] is RP_TABLES_OK no page moves, slot_offs is 0 and
+ * slot_map -1. The entries of live table rows and of the stack are the caller's
+ * and not checked: a page that they hold twice is handed out twice. */
+rp_status rp_page_tables_resize(const rp_page_tables* tables, const int32_t* old_lens, const int32_t* new_lens,
+                                int32_t* status, int32_t* slot_offs, int32_t* slot_map, int32_t max_slots,
+                                hipStream_t stream);
+
+/* Write rows of k_new and v_new (bf16 [num_src][Hkv][head_dim], 16-byte aligned)
+ * into the slots of a list: entry i < num_tokens puts row src_rows[i] (row i
+ * where src_rows is NULL) into slot_map[i]. Entries whose slot is not in
+ * [0, num_pages * 16) or whose row is not in [0, num_src) are skipped; -1 pads.
+ * A row may be written to several slots, a slot must not occur twice.
+ * RP_KV_BF16: the values are copied.
+ * RP_KV_FP8_E4M3: a run is a maximal stretch of entries whose slots follow each
+ * other (slot + 1) inside one page; a page must have at most one run. Per run
+ * and kv-head, separately for K and V, in fp32: amax = max |x| over the run's
+ * rows; a run that begins in row 0 sets scale = amax / 448 (1 if amax == 0); one
+ * that begins in row r > 0 keeps the scale if amax <= 448 * scale, and otherwise
+ * sets scale = amax / 448 and requantises rows 0..r-1 from code * old_scale;
+ * rows are stored as e4m3(x / scale), rounding and NaN as rp_kv_append's. A run
+ * of one row is rp_kv_append's rule, a run from row 0 rp_prefill_kv_write's.
+ * Repeating a call with the same inputs is idempotent. */
+rp_status rp_kv_write_slots(const rp_paged_kv* kv, const int32_t* slot_map, int32_t num_tokens, const void* k_new,
+                            const void* v_new, const int32_t* src_rows, int32_t num_src, hipStream_t stream);
+
 /* ---- Shared-prefix prefill ---------------------------------------------
  * Every response of a GRPO group is sampled from the same prompt (paper,
  * Section 2.1), so a prompt is processed once per group, not once per

@@ -12,6 +12,8 @@ Everything is computed in float64 from the plain definitions:
 * the log-sum-exp merge of partial results over disjoint key subsets;
 * the KV append (bf16 copy, or OCP e4m3fn quantisation with a per-(page, head)
   scale);
+* the attention of trees of drafted tokens, K/V rows written by slot, and block
+  tables grown and shrunk from lengths;
 * the shared-prefix prefill: causal attention over each group's prompt and
   the one-time write of its K/V pages;
 * the pre-attention side of a decode step: RMS norm and rotary embedding of
@@ -31,10 +33,12 @@ from .append import kv_append, append_for_workload
 from .prefill import prefill_attention, prefill_kv_write
 from .qkprep import decode_positions, decode_step_prep, qk_prep, rms_norm, rope
 from .sched import simulate as simulate_schedule
+from .slots import kv_write_slots, page_tables_resize
+from .tree import tree_attention, tree_for_workload
 from .grpo import advantage, advantage_f32, group_stats
 
 __all__ = ["bf16_to_f64", "bf16_to_f32", "e4m3_to_f64", "e4m3_encode", "E4M3_MAX",
            "decode_attention", "key_slots", "attention_for_workload",
            "lse_combine", "kv_append", "append_for_workload", "prefill_attention", "prefill_kv_write",
            "decode_positions", "decode_step_prep", "qk_prep", "rms_norm", "rope",
-           "simulate_schedule", "advantage", "advantage_f32", "group_stats"]
+           "kv_write_slots", "page_tables_resize", "tree_attention", "tree_for_workload", "simulate_schedule", "advantage", "advantage_f32", "group_stats"]

@@ -31,7 +31,10 @@ EXPORTED = ("rp_status_string", "rp_last_error", "rp_kv_append",
             "rp_plan", "rp_attn_parts", "rp_combine_parts", "rp_plan_layout", "rp_validate_layout",
             "rp_prefill_kv_write", "rp_prefill_attn", "rp_decode_qk_prep", "rp_sched_simulate",
             "rp_grpo_advantage", "rp_prefill", "rp_group_decode_attn_noalloc", "rp_decode_qk_prep_plan",
-            "rp_selftest_mfma", "rp_stream_read")
+            "rp_selftest_mfma", "rp_stream_read", "rp_group_tree_attn_workspace_size", "rp_group_tree_attn",
+            "rp_kv_write_slots", "rp_page_tables_resize")
+# include/rp.h rp_tables_status, as the device's status[0] holds it
+RP_TABLES_OK, RP_TABLES_NO_PAGES, RP_TABLES_BAD_LENGTH, RP_TABLES_NO_SLOTS, RP_TABLES_BAD_FREE_LIST = range(5)
 RP_STREAM_READ_SINK_WORDS = 2048 * 4   # include/rp.h
 # include/rp.h rp_selftest_shape: name -> (code, M, N, K)
 RP_SELFTEST_SHAPES = {"16x16x32": (0, 16, 16, 32), "16x16x16": (1, 16, 16, 16), "16x16x32_lds_tr": (2, 16, 16, 32)}
@@ -59,6 +62,17 @@ class RpPrefillLayout(ctypes.Structure):
     _fields_ = [("num_groups", ctypes.c_int32), ("num_q_heads", ctypes.c_int32), ("num_tokens", ctypes.c_int32),
                 ("prompt_offs", ctypes.c_void_p), ("prefix_block_table", ctypes.c_void_p),
                 ("max_prefix_pages", ctypes.c_int32)]
+
+
+class RpDraftTree(ctypes.Structure):
+    _fields_ = [("num_drafts", ctypes.c_int32), ("max_drafts", ctypes.c_int32), ("draft_offs", ctypes.c_void_p),
+                ("masks", ctypes.c_void_p)]
+
+
+class RpPageTables(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("block_table", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
+                ("free_count", ctypes.c_void_p)]
 
 
 class RpPlanInfo(ctypes.Structure):
@@ -122,6 +136,10 @@ def load() -> ctypes.CDLL:
         "rp_sched_simulate": (ctypes.c_int, [P, P, P, P, P, P, P, P, P, P]),
         "rp_grpo_advantage": (ctypes.c_int, [P, I32, I32, ctypes.c_double, I32, P, P, P, P]),
         "rp_selftest_mfma": (ctypes.c_int, [I32, P, P, P, P]),
+        "rp_group_tree_attn_workspace_size": (ctypes.c_int, [P, P, P, ctypes.POINTER(ctypes.c_size_t)]),
+        "rp_group_tree_attn": (ctypes.c_int, [P, P, P, P, P, P, F32, P, P, P, ctypes.c_size_t, P]),
+        "rp_kv_write_slots": (ctypes.c_int, [P, P, I32, P, P, P, I32, P]),
+        "rp_page_tables_resize": (ctypes.c_int, [P, P, P, P, P, P, I32, P]),
         "rp_stream_read": (ctypes.c_int, [P, ctypes.c_uint64, P, I32, P]),
     }
     for name, (res, args) in sig.items():
@@ -291,6 +309,83 @@ def plan_layout(kv, layout) -> RpPlanInfo:
 def validate_layout(kv, layout, stream=None) -> None:
     _check(load().rp_validate_layout(ctypes.byref(kv), ctypes.byref(layout), _stream(stream)),
            "rp_validate_layout")
+
+
+def _tensors(*specs) -> None:
+    """Refuse tensors that the library would read as others: (name, tensor, dtype, shape), with None for a size
+    that may be any. Raw addresses (int) and None pass; every tensor is on the current device."""
+    for name, t, dtype, shape in specs:
+        if t is None or isinstance(t, int):
+            continue
+        if t.dtype is not dtype:
+            raise ValueError(f"{name}: dtype {t.dtype}, not {dtype}")
+        if t.shape != shape and (t.dim() != len(shape) or any(w not in (None, g) for g, w in zip(t.shape, shape))):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, not {shape}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous (strides {t.stride()})")
+        if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+            raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+
+
+def draft_tree(draft_offs, masks, *, max_drafts, num_drafts=None) -> RpDraftTree:
+    """Describe packed trees: sequence s has the drafts draft_offs[s] .. draft_offs[s+1]-1 (int32 [S + 1]),
+    masks (int64 or uint64 [T]) say which drafts of its sequence each one sees, bit u for the u-th."""
+    _tensors(("draft_offs", draft_offs, torch.int32, (None,)),
+             ("masks", masks, torch.uint64 if getattr(masks, "dtype", None) is torch.uint64 else torch.int64, (None,)))
+    return RpDraftTree(int(masks.shape[0]) if num_drafts is None else int(num_drafts), int(max_drafts),
+                       _ptr(draft_offs), _ptr(masks))
+
+
+def group_tree_attn_workspace_size(kv, layout, tree) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().rp_group_tree_attn_workspace_size(ctypes.byref(kv), ctypes.byref(layout), ctypes.byref(tree),
+                                                    ctypes.byref(n)), "rp_group_tree_attn_workspace_size")
+    return int(n.value)
+
+
+def group_tree_attn(kv, layout, tree, q, k_draft, v_draft, softmax_scale, out, lse, workspace, stream=None) -> None:
+    """Attention of every drafted token over the cache and its tree: q, out bf16 [T][Hq][d], k_draft, v_draft
+    bf16 [T][Hkv][d], lse fp32 [T][Hq] or None, workspace uint8 (None where its size is 0)."""
+    T, hq, hkv, d = tree.num_drafts, layout.num_q_heads, kv.num_kv_heads, kv.head_dim
+    bf16 = torch.bfloat16
+    _tensors(("q", q, bf16, (T, hq, d)), ("k_draft", k_draft, bf16, (T, hkv, d)), ("v_draft", v_draft, bf16, (T, hkv, d)),
+             ("out", out, bf16, (T, hq, d)), ("lse", lse, torch.float32, (T, hq)))
+    _check(load().rp_group_tree_attn(ctypes.byref(kv), ctypes.byref(layout), ctypes.byref(tree), _ptr(q),
+                                     _ptr(k_draft), _ptr(v_draft), float(softmax_scale), _ptr(out), _ptr(lse),
+                                     _ptr(workspace), _ws_bytes(workspace), _stream(stream)), "rp_group_tree_attn")
+
+
+def page_tables(block_table, free_pages, free_count) -> RpPageTables:
+    """Describe block tables (int32 [S][max_pages]) and their stack of free pages (int32 [num_pages], and its
+    count, int32 [1])."""
+    _tensors(("block_table", block_table, torch.int32, (None, None)), ("free_pages", free_pages, torch.int32, (None,)),
+             ("free_count", free_count, torch.int32, (1,)))
+    return RpPageTables(int(block_table.shape[0]), int(block_table.shape[1]), 16, int(free_pages.shape[0]),
+                        _ptr(block_table), _ptr(free_pages), _ptr(free_count))
+
+
+def page_tables_resize(tables, old_lens, new_lens, status, slot_offs=None, slot_map=None, stream=None) -> None:
+    """Grow and shrink sequences: int32 [S] lengths before and after; status int32 [4] on the device gets
+    {RP_TABLES_*, pages taken, pages given back, new tokens}; slot_offs int32 [S + 1]; slot_map int32 [max_slots]."""
+    S, i32 = tables.num_seqs, torch.int32
+    _tensors(("old_lens", old_lens, i32, (S,)), ("new_lens", new_lens, i32, (S,)), ("status", status, i32, (4,)),
+             ("slot_offs", slot_offs, i32, (S + 1,)), ("slot_map", slot_map, i32, (None,)))
+    slots = 0 if slot_map is None else int(slot_map.shape[0])
+    # An empty tensor has no address; the library then only counts against its size.
+    where = (_ptr(slot_map) or _ptr(slot_offs)) if slot_map is not None else None
+    _check(load().rp_page_tables_resize(ctypes.byref(tables), _ptr(old_lens), _ptr(new_lens), _ptr(status),
+                                        _ptr(slot_offs), where, slots, _stream(stream)), "rp_page_tables_resize")
+
+
+def kv_write_slots(kv, slot_map, k_new, v_new, src_rows=None, stream=None) -> None:
+    """Write rows of k_new and v_new (bf16 [num_src][Hkv][d]) into the slots of slot_map (int32 [T]): row
+    src_rows[i] (int32 [T]; row i where None) into slot_map[i]; negative slots are skipped."""
+    T, rows = int(slot_map.shape[0]), int(k_new.shape[0])
+    row = (rows, kv.num_kv_heads, kv.head_dim)
+    _tensors(("slot_map", slot_map, torch.int32, (T,)), ("k_new", k_new, torch.bfloat16, row),
+             ("v_new", v_new, torch.bfloat16, row), ("src_rows", src_rows, torch.int32, (T,)))
+    _check(load().rp_kv_write_slots(ctypes.byref(kv), _ptr(slot_map), T, _ptr(k_new), _ptr(v_new), _ptr(src_rows),
+                                    rows, _stream(stream)), "rp_kv_write_slots")
 
 
 def prefill_layout(prompt_offs, prefix_block_table, *, num_q_heads, num_tokens) -> RpPrefillLayout:

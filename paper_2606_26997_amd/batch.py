@@ -95,6 +95,28 @@ class DeviceBatch:
             self.kv_append(stream)
         self.attention(stream)
 
+    # -- trees of drafted tokens ------------------------------------------------
+    def set_drafts(self, draft_offs, masks, q, k_draft, v_draft, *, max_drafts):
+        """Drafted tokens of every sequence, packed (see ``draft_tree``), for ``tree_attention`` over the
+        ``resp_lens`` cached tokens."""
+        d = self.device
+        self.draft_offs, self.draft_masks = _dev(draft_offs, d, torch.int32), _dev(masks, d, torch.int64)
+        self.draft_q, self.k_draft, self.v_draft = _dev(q, d), _dev(k_draft, d), _dev(v_draft, d)
+        self.tree = B.draft_tree(self.draft_offs, self.draft_masks, max_drafts=max_drafts)
+        self.draft_out = torch.zeros_like(self.draft_q)
+        self.draft_lse = torch.zeros(self.draft_q.shape[:2], dtype=torch.float32, device=d)
+        ws = B.group_tree_attn_workspace_size(self.kv, self.append_layout, self.tree)
+        self.draft_workspace = torch.empty(max(ws, 256), dtype=torch.uint8, device=d)
+
+    def tree_attention(self, stream=None):
+        """Attention of the drafts over the cached tokens and their trees (``draft_out``, ``draft_lse``)."""
+        B.group_tree_attn(self.kv, self.append_layout, self.tree, self.draft_q, self.k_draft, self.v_draft,
+                          self.softmax_scale, self.draft_out, self.draft_lse, self.draft_workspace, stream)
+
+    def write_slots(self, slot_map, k_new, v_new, src_rows=None, stream=None):
+        """Rows of k_new and v_new into slots of the batch's pool (accepted drafts, say)."""
+        B.kv_write_slots(self.kv, slot_map, k_new, v_new, src_rows, stream)
+
     # -- decode step from the raw projections ---------------------------------
     def set_projections(self, q_in, k_in, v_in, q_norm_w, k_norm_w, *, rms_eps=1e-6, rope_theta=1e6,
                         keep_k=False):
@@ -153,6 +175,33 @@ class DeviceBatch:
 
     def validate(self, stream=None):
         B.validate_layout(self.kv, self.attn_layout, stream)
+
+
+class PageTables:
+    """Block tables of up to ``num_seqs`` sequences (or prefixes) on the device, their lengths, and the stack of
+    a pool's free pages. Tables of one pool share its stack: pass ``stack`` of the first one to the others."""
+
+    def __init__(self, *, num_seqs, max_pages, num_pages=None, stack=None, device="cuda"):
+        d = torch.device(device)
+        self.block_table = torch.full((num_seqs, max_pages), -1, dtype=torch.int32, device=d)
+        self.lens = torch.zeros(num_seqs, dtype=torch.int32, device=d)
+        if stack is None:
+            # The first pages are on top.
+            stack = (torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=d),
+                     torch.full((1,), num_pages, dtype=torch.int32, device=d))
+        self.stack = stack
+        self.status = torch.zeros(4, dtype=torch.int32, device=d)
+        self.slot_offs = torch.zeros(num_seqs + 1, dtype=torch.int32, device=d)
+        self.tables = B.page_tables(self.block_table, *stack)
+
+    def resize(self, new_lens, slot_map=None, stream=None):
+        """Take and give back pages for ``new_lens`` (int32 [num_seqs], on the device). ``status`` says on the
+        device whether it was done; the lengths follow only then, and ``slot_map`` has the new tokens' slots."""
+        B.page_tables_resize(self.tables, self.lens, new_lens, self.status, self.slot_offs, slot_map, stream)
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream)
+        with torch.cuda.stream(stream):  # None: the current one
+            self.lens.copy_(torch.where(self.status[0] == B.RP_TABLES_OK, new_lens, self.lens))
 
 
 class PrefillBatch:

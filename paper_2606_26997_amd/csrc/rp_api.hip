@@ -343,6 +343,56 @@ rp_status qk_prep_args(const rp_paged_kv* kv, const rp_group_layout* l, const Sh
   return RP_OK;
 }
 
+// How a tree attention is divided, from host scalars alone.
+struct TreePlan {
+  bool whole;
+  int tiles, row_blocks, chunk, max_pc, piece, max_pieces, ppr, repeats;
+  long long prefix_blocks, blocks;
+  size_t parts, part_o, part_lse, total;
+};
+
+rp_status check_tree(const Shape& sh, const rp_draft_tree* t) {
+  if (t == nullptr) return fail(RP_ERR_INVALID_ARG, "tree is NULL");
+  if (t->num_drafts < 0) return fail(RP_ERR_INVALID_ARG, "num_drafts must be >= 0");
+  if (t->max_drafts < 1) return fail(RP_ERR_INVALID_ARG, "max_drafts must be >= 1");
+  if (t->max_drafts > rp::kTreeMaxDrafts)
+    return fail(RP_ERR_UNSUPPORTED, "max_drafts %d above the limit %d", t->max_drafts, rp::kTreeMaxDrafts);
+  if (sh.S == 0 || t->num_drafts == 0) return RP_OK;
+  if (t->draft_offs == nullptr || !aligned(t->draft_offs, 4))
+    return fail(RP_ERR_INVALID_ARG, "draft_offs must be a non-NULL int32 array");
+  if (t->masks == nullptr || !aligned(t->masks, 8))
+    return fail(RP_ERR_INVALID_ARG, "masks must be a non-NULL uint64 array");
+  return RP_OK;
+}
+
+bool tree_plan(const Shape& sh, const rp_draft_tree* t, TreePlan* p) {
+  const long long T = t->num_drafts;
+  const int rows = t->max_drafts * sh.nrep;
+  p->tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  p->row_blocks = rp::cdiv(rows, 16 * p->tiles);
+  const long long base = (long long)sh.S * sh.Hkv * p->row_blocks;
+  p->whole = sh.max_pp + sh.max_rp <= 64;
+  p->chunk = 32;
+  p->max_pc = rp::cdiv(sh.max_pp, p->chunk);
+  const int want = (int)std::max(1ll, 4096 / base);
+  p->piece = std::min(std::max(rp::cdiv(rp::cdiv(sh.max_rp, want), 16) * 16, 32), rp::kTreeMaxPages);
+  p->max_pieces = p->whole ? 1 : std::max(rp::cdiv(sh.max_rp, p->piece), 1);
+  p->ppr = p->whole ? 0 : p->max_pc + p->max_pieces;
+  const long long per_group = (T * sh.nrep + (long long)sh.G * 16 * p->tiles - 1) / ((long long)sh.G * 16 * p->tiles);
+  p->repeats = (int)std::min(std::max(per_group, 1ll), 64ll);
+  const auto grid = [](long long units, long long repeats) { return (units + 7) / 8 * 8 * repeats; };
+  p->prefix_blocks = p->whole ? 0 : grid((long long)sh.G * p->max_pc * sh.Hkv, p->repeats);
+  p->blocks = p->prefix_blocks + grid((long long)sh.S * sh.Hkv * p->max_pieces, p->row_blocks);
+  if (T * sh.Hq >= (1ll << 31) || T * sh.Hq * std::max(p->ppr, 1) >= (1ll << 31) || p->blocks >= (1ll << 31)) return false;
+  size_t o = 0;
+  const size_t slots = (size_t)T * sh.Hq * p->ppr;
+  p->parts = o;    o = align_up(o + (p->whole ? 0 : sizeof(int) * (size_t)T));
+  p->part_o = o;   o = align_up(o + sizeof(float) * slots * sh.D);
+  p->part_lse = o; o = align_up(o + sizeof(float) * slots);
+  p->total = o;
+  return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -494,6 +544,180 @@ rp_status rp_lse_combine(const float* o_parts, const float* lse_parts, const int
   c.lse = lse_out;
   hipError_t e = rp::launch_combine(c, head_dim, stream);
   return e == hipSuccess ? RP_OK : hip_fail(e, "combine kernel launch");
+}
+
+rp_status rp_group_tree_attn_workspace_size(const rp_paged_kv* kv, const rp_group_layout* l, const rp_draft_tree* tree,
+                                            size_t* bytes) {
+  g_err[0] = 0;
+  if (bytes == nullptr) return fail(RP_ERR_INVALID_ARG, "bytes is NULL");
+  Shape sh;
+  rp_status st = check_shape(kv, l, &sh);
+  if (st == RP_OK) st = check_tree(sh, tree);
+  if (st != RP_OK) return st;
+  *bytes = 0;
+  if (sh.S == 0 || tree->num_drafts == 0) return RP_OK;
+  TreePlan p;
+  if (!tree_plan(sh, tree, &p)) return fail(RP_ERR_UNSUPPORTED, "too many drafts for one call");
+  *bytes = p.total;
+  return RP_OK;
+}
+
+rp_status rp_group_tree_attn(const rp_paged_kv* kv, const rp_group_layout* l, const rp_draft_tree* tree, const void* q,
+                             const void* k_draft, const void* v_draft, float softmax_scale, void* out, float* lse,
+                             void* ws, size_t ws_bytes, hipStream_t stream) {
+  g_err[0] = 0;
+  Shape sh;
+  rp_status st = check_shape(kv, l, &sh);
+  if (st == RP_OK) st = check_tree(sh, tree);
+  if (st != RP_OK) return st;
+  if (!(softmax_scale > 0.f) || !std::isfinite(softmax_scale))
+    return fail(RP_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
+  if (sh.S == 0 || tree->num_drafts == 0) return RP_OK;
+  TreePlan p;
+  if (!tree_plan(sh, tree, &p)) return fail(RP_ERR_UNSUPPORTED, "too many drafts for one call");
+  const void* in[] = {q, k_draft, v_draft, out};
+  for (const void* x : in)
+    if (x == nullptr || !aligned(x, 16))
+      return fail(RP_ERR_INVALID_ARG, "q/k_draft/v_draft/out must be non-NULL and 16-byte aligned");
+  if (lse != nullptr && !aligned(lse, 4)) return fail(RP_ERR_INVALID_ARG, "lse must be 4-byte aligned");
+  if (p.total > 0) {
+    if (ws == nullptr) return fail(RP_ERR_WORKSPACE, "workspace is NULL");
+    if (!aligned(ws, 256)) return fail(RP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    if (ws_bytes < p.total) return fail(RP_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, p.total);
+  }
+  rp::TreeArgs a{};
+  a.k_pages = kv->k_pages;
+  a.v_pages = kv->v_pages;
+  a.k_scale = kv->k_scale;
+  a.v_scale = kv->v_scale;
+  a.num_pages = kv->num_pages;
+  a.num_kv_heads = sh.Hkv;
+  a.num_seqs = sh.S;
+  a.num_groups = sh.G;
+  a.num_q_heads = sh.Hq;
+  a.rep_shift = sh.nrep == 1 ? 0 : sh.nrep == 2 ? 1 : sh.nrep == 4 ? 2 : 3;
+  a.seq_to_group = l->seq_to_group;
+  a.prefix_lens = l->prefix_lens;
+  a.prefix_block_table = l->prefix_block_table;
+  a.max_prefix_pages = sh.max_pp;
+  a.resp_lens = l->resp_lens;
+  a.resp_block_table = l->resp_block_table;
+  a.max_resp_pages = sh.max_rp;
+  a.num_drafts = tree->num_drafts;
+  a.max_drafts = tree->max_drafts;
+  a.draft_offs = tree->draft_offs;
+  a.masks = reinterpret_cast<const unsigned long long*>(tree->masks);
+  a.q = static_cast<const uint16_t*>(q);
+  a.k_draft = static_cast<const uint16_t*>(k_draft);
+  a.v_draft = static_cast<const uint16_t*>(v_draft);
+  a.qk_scale = softmax_scale * rp::kLog2e;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  char* b = static_cast<char*>(ws);
+  if (!p.whole) {
+    a.token_parts = reinterpret_cast<int*>(b + p.parts);
+    a.part_o = reinterpret_cast<float*>(b + p.part_o);
+    a.part_lse = reinterpret_cast<float*>(b + p.part_lse);
+  }
+  a.parts_per_row = p.ppr;
+  a.whole = p.whole ? 1 : 0;
+  a.prefix_chunk = p.chunk;
+  a.max_prefix_chunks = p.max_pc;
+  a.prefix_repeats = p.repeats;
+  a.prefix_blocks = (int)p.prefix_blocks;
+  a.piece_pages = p.piece;
+  a.max_pieces = p.max_pieces;
+  a.row_blocks = p.row_blocks;
+  hipError_t e = rp::launch_tree_attn(a, sh.D, sh.fp8, p.tiles, p.blocks, stream);
+  if (e != hipSuccess) return hip_fail(e, "tree attention kernel launch");
+  if (p.whole) return RP_OK;
+  rp::CombineArgs c{};
+  c.o_parts = a.part_o;
+  c.lse_parts = a.part_lse;
+  c.num_rows = (int)(tree->num_drafts * (long long)sh.Hq);
+  c.out = out;
+  c.lse = lse;
+  c.seq_parts = a.token_parts;
+  c.num_q_heads = sh.Hq;
+  c.parts_per_row = p.ppr;
+  c.live_tokens = a.draft_offs + sh.S;
+  e = rp::launch_combine(c, sh.D, stream);
+  return e == hipSuccess ? RP_OK : hip_fail(e, "combine kernel launch");
+}
+
+rp_status rp_kv_write_slots(const rp_paged_kv* kv, const int32_t* slot_map, int32_t num_tokens, const void* k_new,
+                            const void* v_new, const int32_t* src_rows, int32_t num_src, hipStream_t stream) {
+  g_err[0] = 0;
+  rp_status st = check_kv(kv);
+  if (st != RP_OK) return st;
+  if (num_tokens < 0 || num_src < 0) return fail(RP_ERR_INVALID_ARG, "num_tokens/num_src must be >= 0");
+  if (kv->num_pages >= (1 << 27)) return fail(RP_ERR_UNSUPPORTED, "slots of %d pages pass 32 bits", kv->num_pages);
+  // Blocks of the launch: pieces of 16 bytes, or (bits of the list, kv-head).
+  if ((long long)num_tokens * kv->num_kv_heads * kv->head_dim >= (1ll << 40) ||
+      (long long)num_tokens * kv->num_kv_heads >= (1ll << 30))
+    return fail(RP_ERR_UNSUPPORTED, "too many rows for one call");
+  if (num_tokens == 0 || num_src == 0) return RP_OK;
+  if (slot_map == nullptr || !aligned(slot_map, 4) || !aligned(src_rows, 4))
+    return fail(RP_ERR_INVALID_ARG, "slot_map (non-NULL) and src_rows must be int32 arrays");
+  if (k_new == nullptr || v_new == nullptr || !aligned(k_new, 16) || !aligned(v_new, 16))
+    return fail(RP_ERR_INVALID_ARG, "k_new/v_new must be non-NULL and 16-byte aligned");
+  rp::WriteArgs a;
+  a.k_pages = kv->k_pages;
+  a.v_pages = kv->v_pages;
+  a.k_scale = kv->k_scale;
+  a.v_scale = kv->v_scale;
+  a.num_slots = kv->num_pages * rp::kPage;
+  a.num_kv_heads = kv->num_kv_heads;
+  a.num_tokens = num_tokens;
+  a.num_src = num_src;
+  a.slot_map = slot_map;
+  a.src_rows = src_rows;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.chunk = 16;
+  hipError_t e = rp::launch_write_slots(a, kv->head_dim, rp::enum_bits(kv->kv_dtype) == RP_KV_FP8_E4M3, stream);
+  return e == hipSuccess ? RP_OK : hip_fail(e, "slot write kernel launch");
+}
+
+rp_status rp_page_tables_resize(const rp_page_tables* t, const int32_t* old_lens, const int32_t* new_lens,
+                                int32_t* status, int32_t* slot_offs, int32_t* slot_map, int32_t max_slots,
+                                hipStream_t stream) {
+  g_err[0] = 0;
+  if (t == nullptr) return fail(RP_ERR_INVALID_ARG, "tables is NULL");
+  if (t->num_seqs < 0 || t->max_pages < 0 || t->num_pages < 1 || max_slots < 0)
+    return fail(RP_ERR_INVALID_ARG, "num_seqs/max_pages/max_slots must be >= 0 and num_pages >= 1");
+  if (t->page_size != rp::kPage) return fail(RP_ERR_UNSUPPORTED, "page_size %d unsupported (16 only)", t->page_size);
+  if (t->num_seqs > rp::kTableMaxSeqs)
+    return fail(RP_ERR_UNSUPPORTED, "num_seqs %d above the limit %d", t->num_seqs, rp::kTableMaxSeqs);
+  if (t->num_pages >= (1 << 27) || t->max_pages >= (1 << 27) || (long long)t->num_seqs * t->max_pages >= (1ll << 31))
+    return fail(RP_ERR_UNSUPPORTED, "tables too large for int32 slots");
+  if (status == nullptr || !aligned(status, 4)) return fail(RP_ERR_INVALID_ARG, "status must be a non-NULL int32 array");
+  if (t->free_count == nullptr || t->free_pages == nullptr || !aligned(t->free_count, 4) || !aligned(t->free_pages, 4))
+    return fail(RP_ERR_INVALID_ARG, "free_pages/free_count must be non-NULL int32 arrays");
+  if (slot_map != nullptr && slot_offs == nullptr) return fail(RP_ERR_INVALID_ARG, "slot_map needs slot_offs");
+  if (!aligned(slot_map, 4) || !aligned(slot_offs, 4))
+    return fail(RP_ERR_INVALID_ARG, "slot_map/slot_offs must be int32 arrays");
+  if (t->num_seqs > 0) {
+    if (old_lens == nullptr || new_lens == nullptr || !aligned(old_lens, 4) || !aligned(new_lens, 4))
+      return fail(RP_ERR_INVALID_ARG, "old_lens/new_lens must be non-NULL int32 arrays");
+    if (t->max_pages > 0 && (t->block_table == nullptr || !aligned(t->block_table, 4)))
+      return fail(RP_ERR_INVALID_ARG, "block_table must be a non-NULL int32 array");
+  }
+  rp::TableArgs a;
+  a.num_seqs = t->num_seqs;
+  a.max_pages = t->max_pages;
+  a.num_pages = t->num_pages;
+  a.max_slots = slot_map != nullptr ? max_slots : 0;
+  a.block_table = t->block_table;
+  a.free_pages = t->free_pages;
+  a.free_count = t->free_count;
+  a.old_lens = old_lens;
+  a.new_lens = new_lens;
+  a.slot_offs = slot_offs;
+  a.slot_map = slot_map;
+  a.status = status;
+  hipError_t e = rp::launch_page_tables(a, 1, stream);
+  return e == hipSuccess ? RP_OK : hip_fail(e, "page table kernel launch");
 }
 
 rp_status rp_kv_append(const rp_paged_kv* kv, const rp_group_layout* l, const void* k_new, const void* v_new,

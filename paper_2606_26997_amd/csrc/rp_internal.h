@@ -66,6 +66,9 @@ struct CombineArgs {
   // planned slots only: parts per query row of each sequence, from the plan
   const int* seq_parts;
   int num_q_heads, parts_per_row;
+  // tree attention only (seq_parts then counts each token's parts): rows of
+  // tokens from *live_tokens on, and rows without parts, are left as they are
+  const int* live_tokens;
 };
 
 struct AppendArgs {
@@ -140,6 +143,81 @@ struct PrefillArgs {
   int write_pages;  // attention kernel also writes the K/V pages (one launch for the whole prefill)
 };
 
+// Waves of a workgroup of the tree attention, and the most pages its units
+// take: a wave holds the page ids of its share, 128 at most, and a share is a
+// quarter of the unit's pages and of its (at most four) blocks of drafts.
+constexpr int kTreeWaves = 4;
+constexpr int kTreeMaxPages = 480;
+constexpr int kTreeMaxDrafts = 64;
+
+// Attention of trees of drafted tokens over the cache.
+struct TreeArgs {
+  const void* k_pages;
+  const void* v_pages;
+  const float* k_scale;
+  const float* v_scale;
+  int num_pages, num_kv_heads;
+  int num_seqs, num_groups, num_q_heads;
+  int rep_shift;  // log2(num_q_heads / num_kv_heads)
+  const int* seq_to_group;
+  const int* prefix_lens;
+  const int* prefix_block_table;
+  int max_prefix_pages;
+  const int* resp_lens;
+  const int* resp_block_table;
+  int max_resp_pages;
+  int num_drafts, max_drafts;
+  const int* draft_offs;             // [S + 1]
+  const unsigned long long* masks;   // [T]
+  const uint16_t* q;                 // bf16 [T][Hq][D]
+  const uint16_t* k_draft;           // bf16 [T][Hkv][D]
+  const uint16_t* v_draft;
+  float qk_scale;                    // softmax_scale * log2(e)
+  uint16_t* out;                     // bf16 [T][Hq][D]
+  float* lse;                        // [T][Hq] or null
+  // Partial results (not in the whole form): row r's in slots r * parts_per_row
+  // + k, its prefix chunks first, then its response's pieces.
+  float* part_o;
+  float* part_lse;
+  int* token_parts;                  // [T] partial results of each row of a token, 0: it is stored already
+  int parts_per_row;
+  // How the launch is divided.
+  int whole;                         // a unit takes all keys of its rows
+  int prefix_chunk, max_prefix_chunks, prefix_repeats, prefix_blocks;
+  int piece_pages, max_pieces, row_blocks;
+};
+
+// K/V rows into the cache by slot.
+struct WriteArgs {
+  void* k_pages;
+  void* v_pages;
+  float* k_scale;
+  float* v_scale;
+  int num_slots;          // num_pages * 16
+  int num_kv_heads;
+  int num_tokens, num_src;
+  const int* slot_map;    // [num_tokens]
+  const int* src_rows;    // [num_tokens] or null: row i
+  const void* k_new;      // bf16 [num_src][Hkv][D]
+  const void* v_new;
+  int chunk;              // fp8: list entries per wave, at most 48
+};
+
+// Most sequences of a resize: their prefix sums stay in LDS.
+constexpr int kTableMaxSeqs = 4096;
+
+struct TableArgs {
+  int num_seqs, max_pages, num_pages, max_slots;
+  int* block_table;   // [S][max_pages]
+  int* free_pages;    // [num_pages], a stack
+  int* free_count;    // [1]
+  const int* old_lens;
+  const int* new_lens;
+  int* slot_offs;     // [S + 1] or null
+  int* slot_map;      // [max_slots] or null
+  int* status;        // [4]
+};
+
 struct ValidateArgs {
   int num_pages, num_seqs, num_groups;
   const int* seq_to_group;
@@ -164,6 +242,11 @@ hipError_t launch_attn_parts(const AttnArgs& a, int head_dim, int n_rep, bool fp
 hipError_t launch_attn_small(const AttnArgs& a, const PlanArgs& p, int head_dim, int n_rep, bool fp8, void* out,
                              float* lse, hipStream_t stream);
 hipError_t launch_combine(const CombineArgs& a, int head_dim, hipStream_t stream);
+// tiles: 16-column tiles of query rows per unit (1, 2 or 4).
+hipError_t launch_tree_attn(const TreeArgs& a, int head_dim, bool fp8, int tiles, long long blocks, hipStream_t stream);
+hipError_t launch_write_slots(const WriteArgs& a, int head_dim, bool fp8, hipStream_t stream);
+// blocks: workgroups (1: one launch, else two).
+hipError_t launch_page_tables(const TableArgs& a, int blocks, hipStream_t stream);
 hipError_t launch_append(const AppendArgs& a, int head_dim, bool fp8, hipStream_t stream);
 hipError_t launch_prefill_kv_write(const PrefillArgs& a, int head_dim, bool fp8, hipStream_t stream);
 hipError_t launch_prefill_attn(const PrefillArgs& a, int head_dim, int n_rep, hipStream_t stream);
