@@ -343,10 +343,30 @@ rp_status qk_prep_args(const rp_paged_kv* kv, const rp_group_layout* l, const Sh
   return RP_OK;
 }
 
-// How a tree attention is divided, from host scalars alone.
+// Units of a tree attention: two workgroups per compute unit of an MI355X,
+// which read as fast as more of them and leave the shorter end. us a call with
+// 256, 512, 1024 and 2048 units at most (Hq 16, Hkv 8, d 128; sequences x
+// drafts over tokens):
+//   16 x 1-16 over 512 + U[0, 6016]:  55.3  47.9  52.5  55.7
+//   16 x 32 over 512 + U[0, 6016]:    69.0  63.0  73.6  86.2
+//   8 x 8 over 512 + U[0, 16000]:     65.7  62.3  66.0  71.5
+//   16 x 8, fp8, the first's tokens:  42.5  34.9  39.8  43.5
+//   64 x 8 over U[0, 7600]:           197   199   206   199
+//   1 x 8 over 16000:                 25.1  25.9  26.0  25.5
+// A unit below 32 pages costs more in partial results than it gives (the last
+// one with 16-page units 31.8).
+constexpr long long kTreeUnits = 512;
+constexpr int kTreeLeastPages = 32;
+
+// How a tree attention is divided, from host scalars alone. Its forms' lines
+// are at the kernels. Prefixes are either units of their own, read once for all
+// members, or part of every member's pages, read again from the caches: at
+// about 14 TB/s, against the partial results that units of their own write and
+// read, at about 1.2 TB/s, and the second launch where nothing else needs it.
 struct TreePlan {
-  bool whole;
-  int tiles, row_blocks, chunk, max_pc, piece, max_pieces, ppr, repeats;
+  rp::TreeForm form;
+  bool share, ordered;
+  int row_blocks, chunk, max_pc, piece, max_pieces, ppr, repeats;
   long long prefix_blocks, blocks;
   size_t parts, part_o, part_lse, total;
 };
@@ -366,29 +386,51 @@ rp_status check_tree(const Shape& sh, const rp_draft_tree* t) {
 }
 
 bool tree_plan(const Shape& sh, const rp_draft_tree* t, TreePlan* p) {
-  const long long T = t->num_drafts;
+  using rp::TreeForm;
+  const long long T = t->num_drafts, pairs = (long long)sh.S * sh.Hkv;
   const int rows = t->max_drafts * sh.nrep;
-  p->tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  p->row_blocks = rp::cdiv(rows, 16 * p->tiles);
-  const long long base = (long long)sh.S * sh.Hkv * p->row_blocks;
-  p->whole = sh.max_pp + sh.max_rp <= 64;
-  p->chunk = 32;
-  p->max_pc = rp::cdiv(sh.max_pp, p->chunk);
-  const int want = (int)std::max(1ll, 4096 / base);
-  p->piece = std::min(std::max(rp::cdiv(rp::cdiv(sh.max_rp, want), 16) * 16, 32), rp::kTreeMaxPages);
-  p->max_pieces = p->whole ? 1 : std::max(rp::cdiv(sh.max_rp, p->piece), 1);
-  p->ppr = p->whole ? 0 : p->max_pc + p->max_pieces;
-  const long long per_group = (T * sh.nrep + (long long)sh.G * 16 * p->tiles - 1) / ((long long)sh.G * 16 * p->tiles);
+  p->form = rows <= 16   ? TreeForm::kSplit1
+            : rows <= 32 ? TreeForm::kSplit2
+            : rows <= 64 ? TreeForm::kSplit4
+                         : TreeForm::kRows;
+  const int cols = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128, prefix_cols = rows <= 64 ? 64 : 128;
+  p->row_blocks = rp::cdiv(rows, cols);
+  // Pages of a unit where `count` units of `pages` pages would be the whole
+  // launch: few and long, as many as the chip takes at once.
+  const auto unit_pages = [](int pages, long long count) {
+    const int pieces = (int)std::max(1ll, kTreeUnits / std::max(count, 1ll));
+    return std::min(std::max(rp::cdiv(rp::cdiv(pages, pieces), 16) * 16, kTreeLeastPages), rp::kTreeUnitPages);
+  };
+  const long long base = pairs * p->row_blocks;
+  const long long per_group = (T * sh.nrep + (long long)sh.G * prefix_cols - 1) / ((long long)sh.G * prefix_cols);
   p->repeats = (int)std::min(std::max(per_group, 1ll), 64ll);
+  p->chunk = unit_pages(std::max(sh.max_pp, 1), (long long)sh.G * sh.Hkv * p->repeats);
+  p->max_pc = rp::cdiv(sh.max_pp, p->chunk);
+  // Shared prefixes or not, in us.
+  const int flat_pages = std::max(sh.max_pp + sh.max_rp, 1);
+  const double page_bytes = 2.0 * rp::kPage * sh.D * (sh.fp8 ? 1 : 2);
+  const double again = (sh.S - std::min(sh.G, sh.S)) * (double)sh.max_pp * sh.Hkv * page_bytes / 14e6;
+  const double parts = (double)T * sh.Hq * p->max_pc * sh.D * 8 / 1.2e6 +
+                       (flat_pages <= unit_pages(flat_pages, base) ? 6.0 : 0.0);
+  p->share = again > parts;
+  if (!p->share) p->max_pc = 0;
+  const int pages = p->share ? std::max(sh.max_rp, 1) : flat_pages;
+  p->piece = unit_pages(pages, base);
+  p->max_pieces = rp::cdiv(pages, p->piece);
+  p->ppr = p->max_pc + p->max_pieces;
+  if (p->ppr == 1) p->ppr = 0;  // every result is final
+  p->ordered = base > kTreeUnits && sh.S <= rp::kTreeOrderSeqs;
   const auto grid = [](long long units, long long repeats) { return (units + 7) / 8 * 8 * repeats; };
-  p->prefix_blocks = p->whole ? 0 : grid((long long)sh.G * p->max_pc * sh.Hkv, p->repeats);
-  p->blocks = p->prefix_blocks + grid((long long)sh.S * sh.Hkv * p->max_pieces, p->row_blocks);
-  if (T * sh.Hq >= (1ll << 31) || T * sh.Hq * std::max(p->ppr, 1) >= (1ll << 31) || p->blocks >= (1ll << 31)) return false;
+  p->prefix_blocks = p->share ? grid((long long)sh.G * p->max_pc * sh.Hkv, p->repeats) : 0;
+  p->blocks = p->prefix_blocks + grid(pairs * p->max_pieces, p->row_blocks);
+  const long long slots = T * sh.Hq * p->ppr;
+  if (T * sh.Hq >= (1ll << 31) || slots >= (1ll << 31) || T * sh.Hq * (sh.D / 4) / 256 >= rp::kMaxBlocks256 ||
+      p->blocks > rp::kMaxBlocks256)
+    return false;
   size_t o = 0;
-  const size_t slots = (size_t)T * sh.Hq * p->ppr;
-  p->parts = o;    o = align_up(o + (p->whole ? 0 : sizeof(int) * (size_t)T));
-  p->part_o = o;   o = align_up(o + sizeof(float) * slots * sh.D);
-  p->part_lse = o; o = align_up(o + sizeof(float) * slots);
+  p->parts = o;    o = align_up(o + (p->ppr == 0 ? 0 : sizeof(int) * (size_t)T));
+  p->part_o = o;   o = align_up(o + sizeof(float) * (size_t)slots * sh.D);
+  p->part_lse = o; o = align_up(o + sizeof(float) * (size_t)slots);
   p->total = o;
   return true;
 }
@@ -614,13 +656,13 @@ rp_status rp_group_tree_attn(const rp_paged_kv* kv, const rp_group_layout* l, co
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
   char* b = static_cast<char*>(ws);
-  if (!p.whole) {
+  if (p.ppr > 0) {
     a.token_parts = reinterpret_cast<int*>(b + p.parts);
     a.part_o = reinterpret_cast<float*>(b + p.part_o);
     a.part_lse = reinterpret_cast<float*>(b + p.part_lse);
   }
-  a.parts_per_row = p.ppr;
-  a.whole = p.whole ? 1 : 0;
+  a.share = p.share ? 1 : 0;
+  a.ordered = p.ordered ? 1 : 0;
   a.prefix_chunk = p.chunk;
   a.max_prefix_chunks = p.max_pc;
   a.prefix_repeats = p.repeats;
@@ -628,21 +670,11 @@ rp_status rp_group_tree_attn(const rp_paged_kv* kv, const rp_group_layout* l, co
   a.piece_pages = p.piece;
   a.max_pieces = p.max_pieces;
   a.row_blocks = p.row_blocks;
-  hipError_t e = rp::launch_tree_attn(a, sh.D, sh.fp8, p.tiles, p.blocks, stream);
+  hipError_t e = rp::launch_tree_attn(a, sh.D, sh.fp8, p.form, p.blocks, stream);
   if (e != hipSuccess) return hip_fail(e, "tree attention kernel launch");
-  if (p.whole) return RP_OK;
-  rp::CombineArgs c{};
-  c.o_parts = a.part_o;
-  c.lse_parts = a.part_lse;
-  c.num_rows = (int)(tree->num_drafts * (long long)sh.Hq);
-  c.out = out;
-  c.lse = lse;
-  c.seq_parts = a.token_parts;
-  c.num_q_heads = sh.Hq;
-  c.parts_per_row = p.ppr;
-  c.live_tokens = a.draft_offs + sh.S;
-  e = rp::launch_combine(c, sh.D, stream);
-  return e == hipSuccess ? RP_OK : hip_fail(e, "combine kernel launch");
+  if (p.ppr == 0) return RP_OK;
+  e = rp::launch_tree_merge(a, sh.D, stream);
+  return e == hipSuccess ? RP_OK : hip_fail(e, "tree merge kernel launch");
 }
 
 rp_status rp_kv_write_slots(const rp_paged_kv* kv, const int32_t* slot_map, int32_t num_tokens, const void* k_new,

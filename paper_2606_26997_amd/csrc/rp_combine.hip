@@ -59,7 +59,6 @@ __global__ __launch_bounds__(64 * kCombineWaves) void combine_kernel(const Combi
   } else {
     n = min(max(a.seq_parts[row / a.num_q_heads], 0), a.parts_per_row);
     p0 = row * a.parts_per_row;
-    if (a.live_tokens != nullptr && (n == 0 || row / a.num_q_heads >= *a.live_tokens)) return;
   }
 
   float lp[kBatch];

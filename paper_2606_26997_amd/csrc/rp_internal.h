@@ -66,9 +66,6 @@ struct CombineArgs {
   // planned slots only: parts per query row of each sequence, from the plan
   const int* seq_parts;
   int num_q_heads, parts_per_row;
-  // tree attention only (seq_parts then counts each token's parts): rows of
-  // tokens from *live_tokens on, and rows without parts, are left as they are
-  const int* live_tokens;
 };
 
 struct AppendArgs {
@@ -143,12 +140,20 @@ struct PrefillArgs {
   int write_pages;  // attention kernel also writes the K/V pages (one launch for the whole prefill)
 };
 
-// Waves of a workgroup of the tree attention, and the most pages its units
-// take: a wave holds the page ids of its share, 128 at most, and a share is a
-// quarter of the unit's pages and of its (at most four) blocks of drafts.
+// A launch has fewer than 2^32 threads.
+constexpr long long kMaxBlocks256 = (1ll << 24) - 1;
+
+// Waves of a workgroup of the tree attention, and the forms of its units (keys
+// split between waves of 1 or 2 column tiles; 1 or 2 row tiles per wave over
+// shared keys). Most pages of a unit: in the split form a wave holds the page
+// ids of its share, 128 at most, a quarter of the pages and of the (at most
+// four) blocks of drafts; in the other they are in LDS.
 constexpr int kTreeWaves = 4;
-constexpr int kTreeMaxPages = 480;
+enum class TreeForm { kSplit1, kSplit2, kSplit4, kRows };
+constexpr int kTreeUnitPages = 480;
 constexpr int kTreeMaxDrafts = 64;
+// Most sequences that a launch orders by length.
+constexpr int kTreeOrderSeqs = 1024;
 
 // Attention of trees of drafted tokens over the cache.
 struct TreeArgs {
@@ -175,14 +180,16 @@ struct TreeArgs {
   float qk_scale;                    // softmax_scale * log2(e)
   uint16_t* out;                     // bf16 [T][Hq][D]
   float* lse;                        // [T][Hq] or null
-  // Partial results (not in the whole form): row r's in slots r * parts_per_row
-  // + k, its prefix chunks first, then its response's pieces.
-  float* part_o;
-  float* part_lse;
+  // Partial results (null where every row has one unit): slot k of a row, its
+  // prefix chunks first, then its sequence's pieces, at k * T * Hq + the row's place among
+  // (kv-head, draft, query head of the kv-head), so that a unit's rows follow
+  // each other.
+  float* part_o;                     // [slots][T * Hq][D]
+  float* part_lse;                   // [slots][T * Hq]
   int* token_parts;                  // [T] partial results of each row of a token, 0: it is stored already
-  int parts_per_row;
   // How the launch is divided.
-  int whole;                         // a unit takes all keys of its rows
+  int share;                         // prefixes are units of their own, for all members at once
+  int ordered;                       // sequences by decreasing length
   int prefix_chunk, max_prefix_chunks, prefix_repeats, prefix_blocks;
   int piece_pages, max_pieces, row_blocks;
 };
@@ -242,8 +249,10 @@ hipError_t launch_attn_parts(const AttnArgs& a, int head_dim, int n_rep, bool fp
 hipError_t launch_attn_small(const AttnArgs& a, const PlanArgs& p, int head_dim, int n_rep, bool fp8, void* out,
                              float* lse, hipStream_t stream);
 hipError_t launch_combine(const CombineArgs& a, int head_dim, hipStream_t stream);
-// tiles: 16-column tiles of query rows per unit (1, 2 or 4).
-hipError_t launch_tree_attn(const TreeArgs& a, int head_dim, bool fp8, int tiles, long long blocks, hipStream_t stream);
+// The second launch, unless the form is whole: merges the partial results.
+hipError_t launch_tree_merge(const TreeArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_tree_attn(const TreeArgs& a, int head_dim, bool fp8, TreeForm form, long long blocks,
+                            hipStream_t stream);
 hipError_t launch_write_slots(const WriteArgs& a, int head_dim, bool fp8, hipStream_t stream);
 // blocks: workgroups (1: one launch, else two).
 hipError_t launch_page_tables(const TableArgs& a, int blocks, hipStream_t stream);

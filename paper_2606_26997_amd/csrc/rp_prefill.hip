@@ -15,6 +15,7 @@
 // from the pool), as the prompt's own attention needs no quantised copy.
 #include "rp_device.h"
 #include "rp_internal.h"
+#include "rp_stage.h"
 
 namespace rp {
 namespace {
@@ -154,44 +155,8 @@ __global__ __launch_bounds__(64) void prefill_kv_write_kernel(const PrefillArgs 
 enum PfPages { kPagesNone = 0, kPagesBf16 = 1, kPagesFp8 = 2 };  // what the attention kernel writes besides
 constexpr int kPfWaves = 4;
 constexpr int kPfThreads = 64 * kPfWaves;
-constexpr int kKeyBlk = 32;
 
-// A staged block holds K and V rows as they come from the projections, copied
-// by direct global-to-LDS loads: one instruction of one wave fills a 1 KiB
-// chunk of kRows rows. Row r lies in chunk r % kChunks, slot r / kChunks, and
-// chunks are 32 bytes more than 1 KiB apart, so that the eight rows of a
-// 16-byte K read and the four rows of a transposing V read lie in different
-// banks (no conflict cycles by the counters), at offsets that are immediates of
-// the reads.
-template <int D>
-struct PfSmem {
-  static constexpr int kRows = 512 / D;                 // rows per chunk
-  static constexpr int kChunks = kKeyBlk / kRows;       // chunks of a K (or V) block
-  static constexpr int kPitch = 512 + 16;               // bf16 elements between chunks
-  static constexpr int kElems = kChunks * kPitch;       // a K (or V) block
-  static constexpr int kStage = 2 * kElems;
-  static constexpr int kPerWave = 2 * kChunks / kPfWaves;  // copies per wave and block
-  static_assert(kChunks % kPfWaves == 0, "chunks per wave");
-  __device__ static constexpr int row(int r) { return (r % kChunks) * kPitch + (r / kChunks) * D; }
-};
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-
-// One direct global-to-LDS copy by a whole wave: 16 bytes per lane from
-// base + off to lds + 16 * lane. Written in assembly because the compiler
-// waits for every load in flight before any LDS read that follows its own
-// form of it; pf_wait waits for as many as are needed.
-__device__ inline void pf_copy(uint32_t lds, const uint16_t* base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :
-               : "s"(lds), "v"(off), "s"(base)
-               : "m0", "memory");
-}
-// Waits until at most N of the wave's copies are in flight (and its LDS reads
-// are done), then for the workgroup's other waves.
-template <int N>
-__device__ inline void pf_wait() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
-}
 
 // This wave's copies of one key block. Byte offsets within one prompt's rows
 // fit 32 bits (the host checks it). Rows at or past the prompt's end are read
@@ -199,14 +164,14 @@ __device__ inline void pf_wait() {
 template <int D>
 __device__ inline void pf_load(uint32_t stage, const uint16_t* kbase, const uint16_t* vbase, uint32_t pitch, int u0,
                                int last, int wave, int lane) {
-  using L = PfSmem<D>;
+  using L = KeyStage<D>;
   const int slot = lane / (D / 8), col = (lane % (D / 8)) * 8;
 #pragma unroll
   for (int i = 0; i < L::kPerWave / 2; ++i) {
     const int chunk = wave * (L::kPerWave / 2) + i;
     const uint32_t off = ((uint32_t)min(u0 + slot * L::kChunks + chunk, last) * pitch + (uint32_t)col) * 2u;
-    pf_copy(stage + (uint32_t)(chunk * L::kPitch * 2), kbase, off);
-    pf_copy(stage + (uint32_t)((L::kElems + chunk * L::kPitch) * 2), vbase, off);
+    copy_to_lds(stage + (uint32_t)(chunk * L::kPitch * 2), kbase, off);
+    copy_to_lds(stage + (uint32_t)((L::kElems + chunk * L::kPitch) * 2), vbase, off);
   }
 }
 
@@ -304,7 +269,7 @@ __device__ inline void pf_write_pages_fp8(const PrefillArgs& a, int g, int h, in
 template <int D, int TPB>
 __device__ inline void pf_write_staged(const PrefillArgs& a, int g, int h, int T0, int last, int t, int blk,
                                        const uint16_t* last_blk, const uint16_t* prev_blk) {
-  using L = PfSmem<D>;
+  using L = KeyStage<D>;
   static_assert(TPB <= 2 * kKeyBlk, "the workgroup's rows are staged");
   const int* pbt = a.prefix_block_table + (size_t)g * a.max_prefix_pages;
   const int n = min(TPB, last + 1 - T0) * (D / 8);
@@ -351,7 +316,7 @@ __device__ __forceinline__ void pf_compute(const uint16_t* kst, int u0, float qk
                                            int quad, const int (&tr)[RT], const bf16x8_t (&qop)[RT][D / 32],
                                            f32x4_t (&oacc)[RT][D / 16], f32x4_t (&mneg)[RT], float (&thr)[RT],
                                            float (&lrow)[RT]) {
-  using L = PfSmem<D>;
+  using L = KeyStage<D>;
   constexpr int KB = D / 32, DT = D / 16, ST = kKeyBlk / 16;
   const uint16_t* vst = kst + L::kElems;
   // Entry i of sub-tile st: key u0 + st*16 + quad*4 + i against row r16.
@@ -458,7 +423,7 @@ __device__ __forceinline__ void pf_compute(const uint16_t* kst, int u0, float qk
 template <int D, int NREP, int RT, PfPages WP>
 __global__ __launch_bounds__(kPfThreads) __attribute__((amdgpu_waves_per_eu(RT == 1 ? 4 : 3, 8)))
 void prefill_attn_kernel(const PrefillArgs a, int max_blocks, int stride, int per_set) {
-  using L = PfSmem<D>;
+  using L = KeyStage<D>;
   constexpr int KB = D / 32;              // MFMA k-blocks over head_dim
   constexpr int DT = D / 16;              // 16-column output tiles
   constexpr int TPT = 16 / NREP;          // prompt tokens per 16-row tile
@@ -535,8 +500,8 @@ void prefill_attn_kernel(const PrefillArgs a, int max_blocks, int stride, int pe
   if (nblk > 1) request(1, 1);
   int cur = 0;
   for (int blk = 0; blk < nblk; ++blk) {
-    if ((STAGES == 3 || blk == 0) && blk + 1 < nblk) pf_wait<L::kPerWave>();
-    else pf_wait<0>();
+    if ((STAGES == 3 || blk == 0) && blk + 1 < nblk) wait_copies<L::kPerWave>();
+    else wait_copies<0>();
     if ((STAGES == 3 || blk > 0) && blk + STAGES - 1 < nblk) request(blk + STAGES - 1, cur == 0 ? STAGES - 1 : cur - 1);
     const uint16_t* kst = smem + cur * L::kStage;
     // Blocks wholly below the diagonal for every row of the wave skip the mask.

@@ -9,11 +9,16 @@
 // Query rows (draft, query head of the kv-head) are the columns of
 //   S^T  = K Q^T   on mfma 16x16x32 bf16 (16 tokens x 16 columns x 32 of head_dim)
 //   O^T += V^T P^T on mfma 16x16x16 or 16x16x32 bf16
-// CT tiles of 16 columns share every K and V element that a wave loads.
-// A workgroup's four waves split a unit's keys, walk them independently and
-// merge their states in LDS, so a unit writes one partial result per row.
+// Two forms, by the query rows of a unit of keys:
+//   split  the four waves of a workgroup split a unit's keys, each walks its
+//          share for CT tiles of 16 columns, and their states are merged in
+//          LDS;
+//   rows   the waves share the unit's keys, 32 at a time in LDS, and have RT
+//          tiles of 16 rows each: K and V are read once for 64 RT rows.
+// Group prefixes, whose rows are those of all members, always take the second.
 #include "rp_device.h"
 #include "rp_internal.h"
+#include "rp_stage.h"
 
 namespace rp {
 namespace {
@@ -45,7 +50,9 @@ struct Shape {
   static constexpr int BLOCK_BYTES = kPage * ROW_BYTES;   // one (page, kv-head) block
   static constexpr int EPL = 16 / EB;                     // elements per 16-byte piece
   static constexpr int LOADS = BLOCK_BYTES / 1024;        // pieces per lane and block
-  static constexpr int PAGES = 4 / LOADS;                 // pages per step: 8 KiB of K and V
+  // Pages per step: 8 KiB of K and V, half of that where the scores of four
+  // tiles for them would not fit the registers.
+  static constexpr int PAGES = 4 / LOADS / (FP8 && CT == 4 ? 2 : 1);
   static constexpr int DT = D / 16;
   static constexpr int PITCH = D + 16;                    // staged V row: a transposing read meets no bank twice
   static constexpr int STAGE = PAGES * kPage * PITCH;     // per wave, bf16 elements
@@ -75,76 +82,74 @@ struct Smem {
   unsigned long long mask[16 * CT];
   int row[16 * CT];  // query row (token * Hq + head), -1: unused column
   float m[kWaves][16 * CT], l[kWaves][16 * CT], r[kWaves][16 * CT];
-  int sum[kWaves];
-  int token[16 * CT];
 };
 
 // One wave's state: per tile the output accumulator (lane (r16, quad) of tile
-// t: column r16, elements dt * 16 + quad * 4 + e), the running maximum of the
-// column, and this lane's share of two sums of the probabilities: exact (for
-// the lse), and as rounded to bf16 for the products. The output is normalised
-// by the sum of what was multiplied, so a single dominant key gives its own v;
-// an fp8 page's V scale is in its rounded probabilities, and its rows are
+// t: column r16, elements dt * 16 + quad * 4 + e), minus the column's running
+// maximum (0 until it has one), the threshold over it that moves it (-inf until
+// then), and this lane's share of two sums of the probabilities: exact (for the
+// lse), and as rounded to bf16 for the products. The output is normalised by
+// the sum of what was multiplied, so a single dominant key gives its own v; an
+// fp8 page's V scale is in its rounded probabilities, and its rows are
 // normalised by the exact sum.
-template <int D, bool FP8, int CT>
+template <int D, int T>
 struct State {
-  f32x4_t o[CT][D / 16];
-  float m[CT], l[CT], r[CT];
+  f32x4_t o[T][D / 16];
+  float neg[T], thr[T], l[T], r[T];
+  __device__ void clear() {
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      neg[t] = l[t] = r[t] = 0.f;
+      thr[t] = -INFINITY;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) o[t][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+  }
 };
 
-// Adds N blocks of 16 tokens, scores s (log2 units, -inf where hidden) and
-// staged V, to the state. vs: V scales of the blocks.
-template <int D, bool FP8, int CT, int N, bool SCALED>
-__device__ __forceinline__ void add_blocks(State<D, FP8, CT>& st, f32x4_t (&s)[CT][N], const float (&vs)[N],
-                                           bf16x4_t (&pop)[CT][N]) {
-  constexpr int DT = D / 16;
-  float mx[CT];
-  bool grow = false;
+// The softmax step of tile t over N blocks of 16 keys: scores x (log2 units,
+// less the running maximum, -inf where hidden) become rounded probabilities,
+// times the blocks' V scales vs where SCALED. The maximum moves, and the
+// accumulator is rescaled, only when a score exceeds it by more than the
+// headroom. EXACT: normalised by the exact sum alone.
+template <int D, int T, int N, bool SCALED, bool EXACT>
+__device__ __forceinline__ void softmax_step(State<D, T>& st, int t, f32x4_t (&x)[N], const float (&vs)[N],
+                                             bf16x4_t (&pop)[N]) {
+  float mx = -INFINITY;
 #pragma unroll
-  for (int t = 0; t < CT; ++t) {
-    mx[t] = -INFINITY;
+  for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, x[i][e]);
+  if (__any(mx > st.thr[t])) {
+    mx = max_xor16_32(mx);
+    const float up = mx > st.thr[t] ? mx : 0.f;
+    const float alpha = st.thr[t] == -INFINITY ? 0.f : fast_exp2(-up);  // nothing yet: 0 times it
+    st.thr[t] = mx > st.thr[t] ? kLazyMax : st.thr[t];
+    st.neg[t] -= up;
+    st.l[t] *= alpha;
+    st.r[t] *= alpha;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) mx[t] = fmaxf(mx[t], s[t][i][e]);
-    grow = grow || mx[t] > st.m[t] + kLazyMax;
-  }
-  // The maximum moves, and the accumulator is rescaled, only when a score
-  // exceeds it by more than the headroom.
-  if (__any(grow)) {
+    for (int i = 0; i < N; ++i) x[i] -= up;
 #pragma unroll
-    for (int t = 0; t < CT; ++t) {
-      const float x = max_xor16_32(mx[t]);
-      const float now = x > st.m[t] + kLazyMax ? x : st.m[t];
-      const float alpha = now == st.m[t] ? 1.f : fast_exp2(st.m[t] - now);
-      st.m[t] = now;
-      st.l[t] *= alpha;
-      st.r[t] *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) st.o[t][dt] *= alpha;
-    }
+    for (int dt = 0; dt < D / 16; ++dt) st.o[t][dt] *= alpha;
   }
 #pragma unroll
-  for (int t = 0; t < CT; ++t) {
-    const float mu = st.m[t] == -INFINITY ? 0.f : st.m[t];
+  for (int i = 0; i < N; ++i) {
+    float p[4];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float p[4];
+    for (int e = 0; e < 4; ++e) p[e] = fast_exp2(x[i][e]);
+    st.l[t] += (p[0] + p[1]) + (p[2] + p[3]);
+    if constexpr (SCALED) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) p[e] = fast_exp2(s[t][i][e] - mu);
-      st.l[t] += (p[0] + p[1]) + (p[2] + p[3]);
-      if constexpr (SCALED) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] *= vs[i];
-      }
-      const uint2 w = make_uint2(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]));
-      if constexpr (!FP8) {
-        const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
-        st.r[t] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.x), one, st.r[t], false);
-        st.r[t] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.y), one, st.r[t], false);
-      }
-      pop[t][i] = __builtin_bit_cast(bf16x4_t, w);
+      for (int e = 0; e < 4; ++e) p[e] *= vs[i];
     }
+    const uint2 w = make_uint2(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]));
+    if constexpr (!EXACT) {
+      const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
+      st.r[t] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.x), one, st.r[t], false);
+      st.r[t] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.y), one, st.r[t], false);
+    }
+    pop[i] = __builtin_bit_cast(bf16x4_t, w);
   }
 }
 
@@ -159,17 +164,48 @@ __device__ inline bool not_finite(uint32_t w) {
   return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
 }
 
+// Place of query row `row` among the partial results of a slot.
+__device__ inline size_t part_of(const TreeArgs& a, int row, int slot) {
+  const int t = row / a.num_q_heads, j = row - t * a.num_q_heads;
+  const int h = j >> a.rep_shift, rep = j & ((1 << a.rep_shift) - 1);
+  const size_t rows = (size_t)a.num_drafts * a.num_q_heads;
+  return slot * rows + (((size_t)h * a.num_drafts + t) << a.rep_shift) + rep;
+}
+
+// A lane's part of row `row` (-1: none) of a 16-row tile: elements dt * 16 +
+// quad * 4 + e, as a final result (slot < 0) or as the partial result of a slot.
+template <int D>
+__device__ inline void store_row(const TreeArgs& a, int row, int slot, int quad, const f32x4_t (&o)[D / 16], float inv,
+                                 float lse) {
+  if (row < 0) return;
+  if (slot < 0) {
+    uint16_t* dst = a.out + (size_t)row * D + quad * 4;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) {
+      const f32x4_t x = o[dt] * inv;
+      *reinterpret_cast<uint2*>(dst + dt * 16) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+    }
+    if (a.lse != nullptr && quad == 0) a.lse[row] = lse;
+  } else {
+    const size_t part = part_of(a, row, slot);
+    float* dst = a.part_o + part * D + quad * 4;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4_t*>(dst + dt * 16) = o[dt] * inv;
+    if (quad == 0) a.part_lse[part] = lse;
+  }
+}
+
 // Walks this wave's share of the keys: blocks b0 .. b1 - 1 of the unit, of
-// which the first pages_a + pages_b are pages and the others drafts.
+// which the first pages_a + pages_b are pages and the others drafts. In LDS: vt
+// is the wave's staging area, ql the query rows (where they are there), rows
+// and masks the columns'.
 template <int D, bool FP8, int CT>
-__device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, int b0, int b1,
-                                     Smem<D, FP8, CT>& sm, State<D, FP8, CT>& st) {
+__device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, int b0, int b1, uint16_t* vt,
+                                     const uint16_t* ql, const int* rows, const unsigned long long* masks,
+                                     State<D, CT>& st) {
   using G = Shape<D, FP8, CT>;
   constexpr int EPL = G::EPL, LOADS = G::LOADS, PAGES = G::PAGES, DT = G::DT, PITCH = G::PITCH;
   const int lane = threadIdx.x & 63, r16 = lane & 15, quad = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  uint16_t* vt = reinterpret_cast<uint16_t*>(sm.buf) + wave * G::STAGE;
-  const uint16_t* ql = reinterpret_cast<const uint16_t*>(sm.buf) + kWaves * G::STAGE;
   const int Hkv = a.num_kv_heads;
   const int np = k.pages_a + k.pages_b;
 
@@ -179,7 +215,7 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
   if constexpr (!G::QLDS) {
 #pragma unroll
     for (int t = 0; t < CT; ++t) {
-      const int row = sm.row[t * 16 + r16];
+      const int row = rows[t * 16 + r16];
 #pragma unroll
       for (int j = 0; j < LOADS; ++j)
 #pragma unroll
@@ -243,7 +279,8 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
       for (int i = 0; i < PAGES; ++i) {
         const char* b = vpool + block(p + i);
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) vx[i][j] = *reinterpret_cast<const u32x4_t*>(b + j * 1024);
+        for (int j = 0; j < LOADS; ++j)
+          vx[i][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(b + j * 1024));
       }
     };
     load_k(0);
@@ -302,7 +339,7 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
 #pragma unroll
         for (int t = 0; t < CT; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[t][i][e] *= km;
+          for (int e = 0; e < 4; ++e) s[t][i][e] = fmaf(s[t][i][e], km, st.neg[t]);
       }
       if (ragged) {
 #pragma unroll
@@ -315,7 +352,8 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
         }
       }
       bf16x4_t pop[CT][PAGES];
-      add_blocks<D, FP8, CT, PAGES, FP8>(st, s, vs, pop);
+#pragma unroll
+      for (int t = 0; t < CT; ++t) softmax_step<D, CT, PAGES, FP8, FP8>(st, t, s[t], vs, pop[t]);
 
       wave_lds_sync();  // the staged V is visible to the whole wave
       if constexpr (PAGES == 1) {
@@ -376,11 +414,11 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
     unsigned long long seen[CT];
 #pragma unroll
     for (int t = 0; t < CT; ++t) {
-      seen[t] = sm.mask[t * 16 + r16] >> u0;
+      seen[t] = masks[t * 16 + r16] >> u0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const bool ok = quad * 4 + e < nv && (seen[t] >> (quad * 4 + e) & 1);
-        s[t][0][e] = ok ? s[t][0][e] * a.qk_scale : -INFINITY;
+        s[t][0][e] = ok ? fmaf(s[t][0][e], a.qk_scale, st.neg[t]) : -INFINITY;
       }
     }
     int odd = 0;  // drafts of the block with such a V row
@@ -401,7 +439,8 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
     }
     bf16x4_t pop[CT][1];
     const float none[1] = {1.f};
-    add_blocks<D, FP8, CT, 1, false>(st, s, none, pop);
+#pragma unroll
+    for (int t = 0; t < CT; ++t) softmax_step<D, CT, 1, false, FP8>(st, t, s[t], none, pop[t]);
     wave_lds_sync();
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
@@ -433,7 +472,7 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
 // A unit: the columns in sm.row over `k`, split between the waves, merged and
 // stored: final rows (slot < 0), or the partial results in their slot.
 template <int D, bool FP8, int CT>
-__device__ __forceinline__ void unit(const TreeArgs& a, const Keys& k, int h, int slot, Smem<D, FP8, CT>& sm) {
+__device__ __forceinline__ void split_unit(const TreeArgs& a, const Keys& k, int h, int slot, Smem<D, FP8, CT>& sm) {
   using G = Shape<D, FP8, CT>;
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -445,25 +484,21 @@ __device__ __forceinline__ void unit(const TreeArgs& a, const Keys& k, int h, in
     }
     __syncthreads();
   }
-  State<D, FP8, CT> st;
-#pragma unroll
-  for (int t = 0; t < CT; ++t) {
-    st.m[t] = -INFINITY;
-    st.l[t] = st.r[t] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < G::DT; ++dt) st.o[t][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
+  State<D, CT> st;
+  st.clear();
   const int blocks = k.pages_a + k.pages_b + cdiv(k.drafts, kPage);
   const int per = cdiv(cdiv(blocks, kWaves), G::PAGES) * G::PAGES;
   const int b0 = min(wave * per, blocks), b1 = min(b0 + per, blocks);
-  if (b0 < b1) walk<D, FP8, CT>(a, k, h, b0, b1, sm, st);
+  uint16_t* buf = reinterpret_cast<uint16_t*>(sm.buf);
+  if (b0 < b1)
+    walk<D, FP8, CT>(a, k, h, b0, b1, buf + wave * G::STAGE, buf + kWaves * G::STAGE, sm.row, sm.mask, st);
 
 #pragma unroll
   for (int t = 0; t < CT; ++t) {
     const float l = xor_sum_from<16>(st.l[t]);
     const float r = FP8 ? l : xor_sum_from<16>(st.r[t]);
     if (quad == 0) {
-      sm.m[wave][t * 16 + r16] = st.m[t];
+      sm.m[wave][t * 16 + r16] = st.thr[t] == -INFINITY ? -INFINITY : -st.neg[t];
       sm.l[wave][t * 16 + r16] = l;
       sm.r[wave][t * 16 + r16] = r;
     }
@@ -484,7 +519,8 @@ __device__ __forceinline__ void unit(const TreeArgs& a, const Keys& k, int h, in
       l += f * sm.l[w][c];
       r += f * sm.r[w][c];
     }
-    const float mine = (st.m[t] == top ? 1.f : fast_exp2(st.m[t] - top)) * (r == 0.f ? 0.f : 1.f / r);
+    const float own = sm.m[wave][c];
+    const float mine = (own == top ? 1.f : fast_exp2(own - top)) * (r == 0.f ? 0.f : 1.f / r);
     if (t > 0) __syncthreads();  // the tile before has been read
 #pragma unroll
     for (int dt = 0; dt < G::DT; ++dt) {
@@ -497,7 +533,7 @@ __device__ __forceinline__ void unit(const TreeArgs& a, const Keys& k, int h, in
       if (slot < 0) {
         if (a.lse != nullptr) a.lse[row] = lse;
       } else {
-        a.part_lse[(size_t)row * a.parts_per_row + slot] = lse;
+        a.part_lse[part_of(a, row, slot)] = lse;
       }
     }
     __syncthreads();
@@ -521,13 +557,320 @@ __device__ __forceinline__ void unit(const TreeArgs& a, const Keys& k, int h, in
 #pragma unroll
         for (int e = 0; e < E; e += 2) dst[e / 2] = pack_bf16x2(x[e], x[e + 1]);
       } else {
-        float4* dst = reinterpret_cast<float4*>(a.part_o + ((size_t)orow * a.parts_per_row + slot) * D + d0);
+        float4* dst = reinterpret_cast<float4*>(a.part_o + part_of(a, orow, slot) * D + d0);
 #pragma unroll
         for (int e = 0; e < E; e += 4) dst[e / 4] = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
       }
     }
   }
 }
+
+// ---- rows form -------------------------------------------------------------
+
+template <int D, bool FP8, int RT>
+struct RowsSmem {
+  static constexpr int STAGES = FP8 ? 2 : 3;
+  static constexpr int COLS = 64 * RT;
+  __attribute__((aligned(16))) uint16_t stage[STAGES * KeyStage<D>::kStage];
+  unsigned long long mask[COLS];
+  int row[COLS];
+  int token[COLS];
+  int sum[kWaves];
+  int odd[kWaves];
+  int page[kTreeUnitPages];                    // page ids of the unit
+  float2 scale[FP8 ? kTreeUnitPages : 1];      // their K scales (times qk_scale) and V scales
+};
+
+// One block of 32 staged keys, two halves of 16 with score scales km and V
+// scales vs (fp8 pages), of which the first n0 and n1 keys count; DRAFTS: those
+// whose bit of `seen` is set. pop: the rounded probabilities. The mask of a
+// ragged block is a branch of its own after the products: a second copy of the
+// whole for it has its LDS reads hoisted and spills 80 registers.
+template <int D, bool FP8, int RT, bool DRAFTS>
+__device__ __forceinline__ void add_rows(const uint16_t* kst, const float (&km)[2], const float (&vs)[2], int n0, int n1,
+                                         const uint32_t (&seen)[RT], const bf16x8_t (&qop)[RT][D / 32],
+                                         State<D, RT>& st, bf16x4_t (&pop)[RT][2]) {
+  using L = KeyStage<D>;
+  constexpr int KB = D / 32, DT = D / 16;
+  constexpr bool SCALED = FP8 && !DRAFTS;
+  const int lane = threadIdx.x & 63, r16 = lane & 15, quad = lane >> 4;
+  f32x4_t s[RT][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    bf16x8_t kop[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+      kop[kb] = *reinterpret_cast<const bf16x8_t*>(kst + L::row(r16) + L::row(i * 16) + kb * 32 + quad * 8);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) s[t][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) s[t][i] = mfma16x16x32(kop[kb], qop[t][kb], s[t][i]);
+  }
+  const uint16_t* vtr = kst + L::kElems + L::row(quad * 4 + r16 / 4) + 4 * (r16 % 4);
+  const auto read_vop = [&](int dt) __attribute__((always_inline)) {
+    const bf16x4_t v0 = lds_read_tr(vtr + dt * 16);
+    const bf16x4_t v1 = lds_read_tr(vtr + L::row(16) + dt * 16);
+    return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  // With one tile there are registers to request V ahead of the softmax.
+  bf16x8_t vpre[DT];
+  if constexpr (RT == 1) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) vpre[dt] = read_vop(dt);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[t][i][e] = fmaf(s[t][i][e], km[i], st.neg[t]);
+        if constexpr (DRAFTS) s[t][i][e] = seen[t] >> (i * 16 + quad * 4 + e) & 1 ? s[t][i][e] : -INFINITY;
+      }
+  if (!DRAFTS && n0 + n1 < 2 * kPage) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[t][0][e] = quad * 4 + e < n0 ? s[t][0][e] : -INFINITY;
+        s[t][1][e] = quad * 4 + e < n1 ? s[t][1][e] : -INFINITY;
+      }
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t) softmax_step<D, RT, 2, SCALED, FP8>(st, t, s[t], vs, pop[t]);
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    const bf16x8_t vo = RT == 1 ? vpre[dt] : read_vop(dt);
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+      st.o[t][dt] =
+          mfma16x16x32(vo, __builtin_shufflevector(pop[t][0], pop[t][1], 0, 1, 2, 3, 4, 5, 6, 7), st.o[t][dt]);
+  }
+}
+
+// A workgroup barrier behind this wave's LDS accesses that leaves its loads in
+// flight (__syncthreads waits for those too).
+__device__ inline void block_sync() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+
+// A unit of at most kTreeUnitPages pages: rows sm.row, RT tiles for each wave. Waves
+// without rows only copy.
+template <int D, bool FP8, int RT>
+__device__ __forceinline__ void rows_unit(const TreeArgs& a, const Keys& k, int h, int slot, RowsSmem<D, FP8, RT>& sm) {
+  using L = KeyStage<D>;
+  constexpr int KB = D / 32, DT = D / 16, STAGES = RowsSmem<D, FP8, RT>::STAGES;
+  constexpr int ROW_BYTES = D * (FP8 ? 1 : 2), BLOCK_BYTES = kPage * ROW_BYTES;
+  const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int Hkv = a.num_kv_heads, np = k.pages_a + k.pages_b, nblk = cdiv(np, 2);
+  const int c0 = wave * RT * 16;
+  const bool active = __builtin_amdgcn_readfirstlane(sm.row[c0]) >= 0;
+
+  bf16x8_t qop[RT][KB];
+  State<D, RT> st;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int row = sm.row[c0 + t * 16 + r16];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+      qop[t][kb] = __builtin_bit_cast(bf16x8_t, piece(a.q + (size_t)max(row, 0) * D + kb * 32 + quad * 8, row >= 0));
+  }
+  st.clear();
+  const uint32_t none[RT] = {};
+  bf16x4_t pop[RT][2];
+
+  if (np > 0) {
+    for (int b = tid; b < np; b += 64 * kWaves) {
+      const int page = clamp_page(b < k.pages_a ? k.table_a[b] : k.table_b[b - k.pages_a], a.num_pages);
+      sm.page[b] = page;
+      if constexpr (FP8) {
+        const size_t at = (size_t)page * Hkv + h;
+        sm.scale[b] = make_float2(a.k_scale[at] * a.qk_scale, a.v_scale[at]);
+      }
+    }
+    // The compiler's wait for the q rows belongs here: inside the loop it would
+    // drain the copies in flight.
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) asm volatile("" : "+v"(qop[t][kb]));
+    __syncthreads();
+    const auto block = [&](int p) __attribute__((always_inline)) {
+      return ((size_t)sm.page[min(p, np - 1)] * Hkv + h) * BLOCK_BYTES;
+    };
+    const auto valid = [&](int p) __attribute__((always_inline)) {
+      const int left = p < k.pages_a ? k.tokens_a - p * kPage : k.tokens_b - (p - k.pages_a) * kPage;
+      return p < np ? min(left, kPage) : 0;
+    };
+    const char* kpool = static_cast<const char*>(a.k_pages);
+    const char* vpool = static_cast<const char*>(a.v_pages);
+    const auto compute = [&](int blk, const uint16_t* kst) __attribute__((always_inline)) {
+      const int n0 = valid(2 * blk), n1 = valid(2 * blk + 1);
+      float km[2], vs[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float2 x = FP8 ? sm.scale[min(2 * blk + i, np - 1)] : make_float2(a.qk_scale, 1.f);
+        km[i] = x.x;
+        vs[i] = x.y;
+      }
+      if (active) add_rows<D, FP8, RT, false>(kst, km, vs, n0, n1, none, qop, st, pop);
+    };
+
+    if constexpr (!FP8) {
+      // Direct copies, STAGES - 1 blocks ahead, one barrier per block.
+      constexpr int CPW = L::kChunks / kWaves, HALF = L::kRows / 2;  // chunks per wave, slots per page
+      const int slot_ = lane / (D / 8);
+      const uint32_t in_page = (uint32_t)(((slot_ % HALF) * L::kChunks + wave * CPW) * ROW_BYTES + lane % (D / 8) * 16);
+      const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)sm.stage;
+      const auto request = [&](int blk, int stage) __attribute__((always_inline)) {
+        const size_t off = block(2 * blk + (slot_ >= HALF ? 1 : 0)) + in_page;
+        const uint32_t to = lds0 + (uint32_t)((stage * L::kStage + wave * CPW * L::kPitch) * 2);
+#pragma unroll
+        for (int i = 0; i < CPW; ++i) copy_to_lds(to + i * L::kPitch * 2, kpool + off + i * ROW_BYTES);
+#pragma unroll
+        for (int i = 0; i < CPW; ++i) copy_to_lds(to + (L::kElems + i * L::kPitch) * 2, vpool + off + i * ROW_BYTES);
+      };
+      request(0, 0);
+      if (nblk > 1) request(1, 1);
+      int cur = 0;
+      for (int blk = 0; blk < nblk; ++blk) {
+        if ((STAGES == 3 || blk == 0) && blk + 1 < nblk) wait_copies<L::kPerWave>();
+        else wait_copies<0>();
+        if ((STAGES == 3 || blk > 0) && blk + STAGES - 1 < nblk) request(blk + STAGES - 1, cur == 0 ? STAGES - 1 : cur - 1);
+        uint16_t* kst = sm.stage + cur * L::kStage;
+        const int n0 = valid(2 * blk), n1 = valid(2 * blk + 1);
+        if (n0 + n1 < 2 * kPage) {  // padding rows may hold anything
+          for (int i = tid; i < kKeyBlk * (D / 8); i += 64 * kWaves) {
+            const int r = i / (D / 8);
+            if (r % kPage >= (r < kPage ? n0 : n1))
+              *reinterpret_cast<u32x4_t*>(kst + L::kElems + L::row(r) + i % (D / 8) * 8) = u32x4_t{0, 0, 0, 0};
+          }
+          __syncthreads();
+        }
+        compute(blk, kst);
+        cur = cur == STAGES - 1 ? 0 : cur + 1;
+      }
+    } else {
+      // Codes go through registers, where they are decoded: 16 bytes of K and
+      // of V for each thread (64-wide heads: of one of them).
+      constexpr int TPR = D / 16;  // threads per row
+      constexpr int DEPTH = 3;  // blocks requested ahead
+      const int part = tid % (kKeyBlk * TPR), r = part / TPR, col = part % TPR * 16;
+      const bool only_v = D == 64 && tid >= kKeyBlk * TPR;
+      u32x4_t ahead[DEPTH][D / 64];
+      const auto load = [&](int blk, u32x4_t (&x)[D / 64]) __attribute__((always_inline)) {
+        const size_t off = block(2 * blk + (r >= kPage ? 1 : 0)) + (uint32_t)(r % kPage * ROW_BYTES + col);
+        x[0] = *reinterpret_cast<const u32x4_t*>((only_v ? vpool : kpool) + off);
+        if constexpr (D == 128) x[1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vpool + off));
+      };
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) load(d, ahead[d]);
+      const auto step = [&](int blk, u32x4_t (&x)[D / 64]) __attribute__((always_inline)) {
+        uint16_t* kst = sm.stage + (blk & 1) * L::kStage;
+        const bool ok = r % kPage < (r < kPage ? valid(2 * blk) : valid(2 * blk + 1));
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          u32x4_t* dst = reinterpret_cast<u32x4_t*>(kst + (only_v || i == 1 ? L::kElems : 0) + L::row(r) + col);
+          const u32x4_t w = ok ? x[i] : u32x4_t{0, 0, 0, 0};
+          dst[0] = decode8(w.x, w.y);
+          dst[1] = decode8(w.z, w.w);
+        }
+        load(blk + DEPTH, x);
+        block_sync();  // the block is there, and the one before has been read
+        compute(blk, kst);
+      };
+      // Whole rounds without a branch between the steps: the compiler's wait
+      // for a step's loads then leaves the later ones in flight.
+      int blk = 0;
+      for (; blk + DEPTH <= nblk; blk += DEPTH) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) step(blk + d, ahead[d]);
+      }
+#pragma unroll
+      for (int d = 0; d < DEPTH - 1; ++d)
+        if (blk + d < nblk) step(blk + d, ahead[d]);
+    }
+  }
+
+  // The drafts, 32 at a time.
+  for (int u0 = 0; u0 < k.drafts; u0 += kKeyBlk) {
+    const int nv = min(k.drafts - u0, kKeyBlk);
+    const size_t first = ((size_t)(k.draft0 + u0) * Hkv + h) * D, stride = (size_t)Hkv * D;
+    constexpr int PER = kKeyBlk * (D / 8) / (64 * kWaves);  // pieces per thread
+    u32x4_t kx[PER], vx[PER];
+    bool bad[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int i = j * 64 * kWaves + tid, r = i / (D / 8), col = i % (D / 8) * 8;
+      kx[j] = piece(a.k_draft + first + r * stride + col, r < nv);
+      vx[j] = piece(a.v_draft + first + r * stride + col, r < nv);
+    }
+    __syncthreads();  // the stages have been read
+    int odd = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int i = j * 64 * kWaves + tid, r = i / (D / 8), col = i % (D / 8) * 8;
+      constexpr int LPT = D / 8, TPL = 64 / LPT;  // lanes per draft, drafts per wave and load
+      bad[j] = not_finite(vx[j].x) || not_finite(vx[j].y) || not_finite(vx[j].z) || not_finite(vx[j].w);
+      const unsigned long long w = __ballot(bad[j]);
+      bool drop = false;
+      if (w != 0) {
+#pragma unroll
+        for (int b = 0; b < TPL; ++b) {
+          const bool is = (w >> (b * LPT) & ((1ull << LPT) - 1)) != 0;
+          drop = drop || (is && lane / LPT == b);
+          odd |= is ? 1 << (j * 64 * kWaves / LPT + wave * TPL + b) : 0;
+        }
+      }
+      *reinterpret_cast<u32x4_t*>(sm.stage + L::row(r) + col) = kx[j];
+      *reinterpret_cast<u32x4_t*>(sm.stage + L::kElems + L::row(r) + col) = drop ? u32x4_t{0, 0, 0, 0} : vx[j];
+    }
+    if (lane == 0) sm.odd[wave] = odd;
+    __syncthreads();
+    odd = sm.odd[0] | sm.odd[1] | sm.odd[2] | sm.odd[3];
+    if (active) {
+      const uint32_t in_tree = nv == 32 ? 0xFFFFFFFFu : (1u << nv) - 1;
+      uint32_t seen[RT];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) seen[t] = (uint32_t)(sm.mask[c0 + t * 16 + r16] >> u0) & in_tree;
+      const float km[2] = {a.qk_scale, a.qk_scale}, vs[2] = {1.f, 1.f};
+      add_rows<D, FP8, RT, true>(sm.stage, km, vs, 0, 0, seen, qop, st, pop);
+      // V rows with an infinity or NaN, for the rows that see them alone: a
+      // weight of zero would not hide them in the product.
+      while (odd != 0) {
+        const int u = __builtin_amdgcn_readfirstlane(__builtin_ctz(odd));
+        odd &= odd - 1;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          const uint2 w = __builtin_bit_cast(uint2, u & 16 ? pop[t][1] : pop[t][0]);
+          const uint32_t word = u & 2 ? w.y : w.x;
+          const float p = __shfl(u & 1 ? bf16_hi(word) : bf16_lo(word), (u >> 2 & 3) * 16 + r16);
+          const bool ok = seen[t] >> u & 1;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            const uint2 x = *reinterpret_cast<const uint2*>(a.v_draft + first + u * stride + dt * 16 + quad * 4);
+            const float v[4] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st.o[t][dt][e] = ok ? fmaf(p, v[e], st.o[t][dt][e]) : st.o[t][dt][e];
+          }
+        }
+      }
+    }
+  }
+
+  if (!active) return;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const float l = xor_sum_from<16>(st.l[t]);
+    const float r = FP8 ? l : xor_sum_from<16>(st.r[t]);
+    store_row<D>(a, sm.row[c0 + t * 16 + r16], slot, quad, st.o[t], r == 0.f ? 0.f : 1.f / r,
+                 l == 0.f ? -INFINITY : (fast_log2(l) - st.neg[t]) * kLn2);
+  }
+}
+
+// ---- units -------------------------------------------------------------------
 
 __device__ inline int2 drafts_of(const TreeArgs& a, int s) {
   const int t0 = min(max(a.draft_offs[s], 0), a.num_drafts);
@@ -537,10 +880,11 @@ __device__ inline int2 drafts_of(const TreeArgs& a, int s) {
 // Columns c0 .. of the drafts of group g, in sequence order: the tokens are
 // found by a scan over the sequences' groups and tree sizes. Returns whether
 // there are any.
-template <int D, bool FP8, int CT>
-__device__ bool group_columns(const TreeArgs& a, int g, int h, int c0, Smem<D, FP8, CT>& sm) {
+template <int D, bool FP8, int RT>
+__device__ bool group_columns(const TreeArgs& a, int g, int h, int c0, RowsSmem<D, FP8, RT>& sm) {
+  constexpr int COLS = RowsSmem<D, FP8, RT>::COLS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int k0 = c0 >> a.rep_shift, k1 = (c0 + 16 * CT) >> a.rep_shift;
+  const int k0 = c0 >> a.rep_shift, k1 = (c0 + COLS) >> a.rep_shift;
   __syncthreads();  // the columns before have been read
   int carry = 0;
   for (int base = 0; base < a.num_seqs && carry < k1; base += 64 * kWaves) {
@@ -564,7 +908,7 @@ __device__ bool group_columns(const TreeArgs& a, int g, int h, int c0, Smem<D, F
     __syncthreads();
   }
   if (carry <= k0) return false;
-  if (tid < 16 * CT) {
+  if (tid < COLS) {
     const int c = c0 + tid, rank = c >> a.rep_shift;
     const int rep = c & ((1 << a.rep_shift) - 1);
     sm.row[tid] = rank < carry ? sm.token[rank - k0] * a.num_q_heads + (h << a.rep_shift) + rep : -1;
@@ -573,115 +917,313 @@ __device__ bool group_columns(const TreeArgs& a, int g, int h, int c0, Smem<D, F
   return true;
 }
 
-// Units of a launch: (group, chunk of prefix pages, kv-head), each several
-// times where a group has many rows, then (sequence, piece of response pages,
-// kv-head, block of rows). Row blocks of one unit follow each other on one XCD
-// (workgroups are dealt to the 8 of them in turn), whose L2 then has the K and
-// V that the first one read. A response's pieces are cut from its end, so its
-// first piece is the short one; pieces are launched from the last to the first
-// and the short ones end the launch. The first piece also takes the drafts.
-// In the whole form a unit takes all keys of its rows, prefix included.
-template <int D, bool FP8, int CT>
-__global__ __launch_bounds__(64 * kWaves) void tree_kernel(const TreeArgs a) {
-  __shared__ Smem<D, FP8, CT> sm;
+// Row blocks of one unit follow each other on one XCD (workgroups are dealt to
+// the 8 of them in turn), whose L2 then has the K and V that the first read.
+__device__ inline void locate(int id, int repeats, int& u, int& r) {
+  const int row = id / (8 * repeats), k = id - row * (8 * repeats);
+  r = k / 8;
+  u = row * 8 + k % 8;
+}
+
+// Workgroup `id` of the group prefixes: (group, chunk of pages, kv-head), each
+// several times where a group has many rows.
+template <int D, bool FP8, int RT>
+__device__ __forceinline__ void prefix_units(const TreeArgs& a, int id, RowsSmem<D, FP8, RT>& sm) {
+  int u, z;
+  locate(id, a.prefix_repeats, u, z);
   const int Hkv = a.num_kv_heads;
-  const auto locate = [](int id, int repeats, int& u, int& r) {
-    const int row = id / (8 * repeats), k = id - row * (8 * repeats);
-    r = k / 8;
-    u = row * 8 + k % 8;
-  };
+  if (u >= a.num_groups * a.max_prefix_chunks * Hkv) return;
+  const int h = u % Hkv, chunk = u / Hkv % a.max_prefix_chunks, g = u / Hkv / a.max_prefix_chunks;
+  const int P = clamp_len(a.prefix_lens[g], a.max_prefix_pages), first = chunk * a.prefix_chunk;
+  const int pages = min(cdiv(P, kPage) - first, a.prefix_chunk);
+  if (pages <= 0) return;
+  Keys k = {};
+  k.table_a = k.table_b = a.prefix_block_table + (size_t)g * a.max_prefix_pages + first;
+  k.pages_a = pages;
+  k.tokens_a = P - first * kPage;
+  for (int rb = z; group_columns<D, FP8, RT>(a, g, h, rb * RowsSmem<D, FP8, RT>::COLS, sm); rb += a.prefix_repeats)
+    rows_unit<D, FP8, RT>(a, k, h, chunk, sm);
+}
+
+// Unit u of the sequences: (piece of pages, sequence, kv-head), its columns from
+// c0 on. A sequence's pieces are cut from its end, so its first piece is the
+// short one; pieces are launched from the last to the first, and the first ones
+// in decreasing order, so that short ones end the launch. The first piece also
+// takes the drafts. Returns false where there is nothing to do.
+struct SeqUnit {
+  Keys k;
+  int h, slot, token0, tokens;  // slot < 0: the result is final
+};
+
+// Pages that the units of sequence s walk: its response's, behind its group's
+// prefix where that is not shared.
+struct SeqPages {
+  int prefix, prefix_tokens, resp, resp_tokens;
+};
+__device__ inline SeqPages seq_pages(const TreeArgs& a, int s, int g) {
+  const int L = clamp_len(a.resp_lens[s], a.max_resp_pages);
+  const int P = clamp_len(a.prefix_lens[g], a.max_prefix_pages);
+  return SeqPages{cdiv(P, kPage), P, cdiv(L, kPage), L};
+}
+// Pages of the first piece, by which sequences are ordered.
+__device__ inline int first_piece(const TreeArgs& a, int s) {
+  const int resp = cdiv(clamp_len(a.resp_lens[s], a.max_resp_pages), kPage);
+  const int n = a.share ? resp : resp + seq_pages(a, s, clamp_group(a.seq_to_group[s], a.num_groups)).prefix;
+  return n <= a.piece_pages ? n : (n - 1) % a.piece_pages + 1;
+}
+
+// The sequence of place `rank` by decreasing first piece (to 1/64 of the
+// longest, then in order): every workgroup sorts the sequences by counting.
+// The workgroup's LDS is not in use yet.
+struct OrderSmem {
+  int count[64], start[64], wave[kWaves], found;
+};
+__device__ int ranked_sequence(const TreeArgs& a, int rank, OrderSmem& m) {
+  constexpr int PER = kTreeOrderSeqs / (64 * kWaves);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int most = a.piece_pages;
+  int bucket[PER];
+  if (tid < 64) m.count[tid] = 0;
+  if (tid == 0) m.found = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int s = i * 64 * kWaves + tid;
+    bucket[i] = -1;
+    if (s < a.num_seqs) {
+      bucket[i] = 63 - first_piece(a, s) * 63 / max(most, 1);
+      atomicAdd(&m.count[bucket[i]], 1);
+    }
+  }
+  __syncthreads();
+  if (tid < 64) {
+    const int n = m.count[tid];
+    int x = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(x, o);
+      x += lane >= o ? y : 0;
+    }
+    m.start[tid] = x - n;
+    if (x - n <= rank && rank < x) m.found = tid;
+  }
+  __syncthreads();
+  const int mine = m.found;
+  int left = rank - m.start[mine];
+  int answer = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (i * 64 * kWaves >= a.num_seqs) break;
+    const unsigned long long in = __ballot(bucket[i] == mine);
+    if (lane == 0) m.wave[wave] = __popcll(in);
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < kWaves; ++w) {
+      before += w < wave ? m.wave[w] : 0;
+      all += m.wave[w];
+    }
+    before += __popcll(in & ((1ull << lane) - 1));
+    __syncthreads();
+    if (bucket[i] == mine && before == left) m.found = i * 64 * kWaves + tid;
+    left -= all;
+  }
+  __syncthreads();
+  answer = m.found;
+  __syncthreads();
+  return answer;
+}
+
+__device__ inline bool seq_unit(const TreeArgs& a, int u, int c0, bool note, OrderSmem& order, SeqUnit& x) {
+  const int Hkv = a.num_kv_heads, per_piece = a.num_seqs * Hkv;
+  const int piece_id = a.max_pieces - 1 - u / per_piece;
+  if (piece_id < 0) return false;
+  x.h = u % Hkv;
+  int s = u % per_piece / Hkv;
+  if (a.ordered && piece_id == 0) s = ranked_sequence(a, s, order);
+  const int2 dr = drafts_of(a, s);
+  x.token0 = dr.x;
+  x.tokens = dr.y;
+  if (c0 >= dr.y << a.rep_shift) return false;
+  const int g = clamp_group(a.seq_to_group[s], a.num_groups);
+  const SeqPages n = seq_pages(a, s, g);
+  const int before = a.share ? 0 : n.prefix, total = before + n.resp;
+  const int pieces = max(cdiv(total, a.piece_pages), 1);
+  if (piece_id >= pieces) return false;
+  const int first = piece_id == 0 ? 0 : total - (pieces - piece_id) * a.piece_pages;
+  const int end = total - (pieces - 1 - piece_id) * a.piece_pages;
+  const int chunks = a.share ? cdiv(n.prefix, a.prefix_chunk) : 0, parts = chunks + pieces;
+  const int a0 = min(first, before), b0 = max(first - before, 0);
+  Keys k = {};
+  k.table_a = a.prefix_block_table + (size_t)g * a.max_prefix_pages + a0;
+  k.pages_a = min(end, before) - a0;
+  k.tokens_a = n.prefix_tokens - a0 * kPage;
+  k.table_b = a.resp_block_table + (size_t)s * a.max_resp_pages + b0;
+  k.pages_b = max(end - before, 0) - b0;
+  k.tokens_b = n.resp_tokens - b0 * kPage;
+  x.slot = parts > 1 ? chunks + piece_id : -1;
+  // Rows whose result is stored at once have no partial results to merge.
+  if (note && a.token_parts != nullptr && piece_id == 0 && x.h == 0 && c0 == 0)
+    for (int i = threadIdx.x & 63; i < dr.y; i += 64) a.token_parts[dr.x + i] = parts > 1 ? parts : 0;
+  if (piece_id == 0) {
+    k.draft0 = dr.x;
+    k.drafts = dr.y;
+  }
+  x.k = k;
+  return true;
+}
+__device__ inline int column_row(const TreeArgs& a, const SeqUnit& x, int c) {
+  const int t = c >> a.rep_shift;
+  return t < x.tokens ? (x.token0 + t) * a.num_q_heads + (x.h << a.rep_shift) + (c & ((1 << a.rep_shift) - 1)) : -1;
+}
+__device__ inline unsigned long long column_mask(const TreeArgs& a, const SeqUnit& x, int c) {
+  const int t = c >> a.rep_shift;
+  return t < x.tokens && x.k.drafts > 0 ? a.masks[x.token0 + t] : 0;
+}
+
+template <int D, bool FP8, int CT>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8))) void tree_split_kernel(const TreeArgs a) {
+  __shared__ union U {
+    Smem<D, FP8, CT> split;
+    Smem<D, FP8, 2> few;
+    RowsSmem<D, FP8, 1> rows;
+    OrderSmem order;
+    __device__ U() {}
+  } sm;
   int id = blockIdx.x;
   if (id < a.prefix_blocks) {
-    int u, z;
-    locate(id, a.prefix_repeats, u, z);
-    if (u >= a.num_groups * a.max_prefix_chunks * Hkv) return;
-    const int h = u % Hkv, chunk = u / Hkv % a.max_prefix_chunks, g = u / Hkv / a.max_prefix_chunks;
-    const int P = clamp_len(a.prefix_lens[g], a.max_prefix_pages), first = chunk * a.prefix_chunk;
-    const int pages = min(cdiv(P, kPage) - first, a.prefix_chunk);
-    if (pages <= 0) return;
-    Keys k = {};
-    k.table_a = k.table_b = a.prefix_block_table + (size_t)g * a.max_prefix_pages + first;
-    k.pages_a = pages;
-    k.tokens_a = P - first * kPage;
-    for (int rb = z; group_columns<D, FP8, CT>(a, g, h, rb * 16 * CT, sm); rb += a.prefix_repeats)
-      unit<D, FP8, CT>(a, k, h, chunk, sm);
+    prefix_units<D, FP8, 1>(a, id, sm.rows);
     return;
   }
   id -= a.prefix_blocks;
   int u, rb;
   locate(id, a.row_blocks, u, rb);
-  const int per_piece = a.num_seqs * Hkv;
-  const int piece_id = a.max_pieces - 1 - u / per_piece;
-  if (piece_id < 0) return;
-  const int s = u % per_piece / Hkv, h = u % Hkv;
-  const int2 dr = drafts_of(a, s);
+  SeqUnit x;
   const int c0 = rb * 16 * CT;
-  if (c0 >= dr.y << a.rep_shift) return;
-  const int g = clamp_group(a.seq_to_group[s], a.num_groups);
-  const int L = clamp_len(a.resp_lens[s], a.max_resp_pages), P = clamp_len(a.prefix_lens[g], a.max_prefix_pages);
-  const int pages = cdiv(L, kPage), prefix_pages = cdiv(P, kPage);
-  Keys k = {};
-  k.table_a = k.table_b = a.resp_block_table + (size_t)s * a.max_resp_pages;
-  int slot = -1;
-  if (a.whole) {
-    k.table_a = a.prefix_block_table + (size_t)g * a.max_prefix_pages;
-    k.pages_a = prefix_pages;
-    k.tokens_a = P;
-    k.pages_b = pages;
-    k.tokens_b = L;
-  } else {
-    const int pieces = max(cdiv(pages, a.piece_pages), 1);
-    if (piece_id >= pieces) return;
-    const int first = piece_id == 0 ? 0 : pages - (pieces - piece_id) * a.piece_pages;
-    const int end = pages - (pieces - 1 - piece_id) * a.piece_pages;
-    const int chunks = cdiv(prefix_pages, a.prefix_chunk);
-    k.table_b += first;
-    k.pages_b = end - first;
-    k.tokens_b = L - first * kPage;
-    if (chunks + pieces > 1) slot = chunks + piece_id;
-    // Rows whose result is stored here have no partial results to merge.
-    if (piece_id == 0 && h == 0)
-      for (int i = threadIdx.x; i < 16 * CT; i += 64 * kWaves) {
-        const int c = c0 + i;
-        if (c < dr.y << a.rep_shift && (c & ((1 << a.rep_shift) - 1)) == 0)
-          a.token_parts[dr.x + (c >> a.rep_shift)] = chunks + pieces > 1 ? chunks + pieces : 0;
-      }
+  if (!seq_unit(a, u, c0, threadIdx.x < 64, sm.order, x)) return;
+  const auto take = [&](auto& m) __attribute__((always_inline)) {
+    constexpr int COLS = sizeof(m.row) / sizeof(int);
+    if ((int)threadIdx.x < COLS) {
+      m.row[threadIdx.x] = column_row(a, x, c0 + threadIdx.x);
+      m.mask[threadIdx.x] = column_mask(a, x, c0 + threadIdx.x);
+    }
+    __syncthreads();
+    split_unit<D, FP8, COLS / 16>(a, x.k, x.h, x.slot, m);
+  };
+  if (CT > 2 && (x.tokens << a.rep_shift) - c0 <= 32) take(sm.few);
+  else take(sm.split);
+}
+
+template <int D, bool FP8, int RT>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
+void tree_rows_kernel(const TreeArgs a) {
+  __shared__ union U {
+    RowsSmem<D, FP8, RT> rows;
+    OrderSmem order;
+    __device__ U() {}
+  } u_;
+  RowsSmem<D, FP8, RT>& sm = u_.rows;
+  constexpr int COLS = RowsSmem<D, FP8, RT>::COLS;
+  int id = blockIdx.x;
+  if (id < a.prefix_blocks) {
+    prefix_units<D, FP8, RT>(a, id, sm);
+    return;
   }
-  if (piece_id == 0) {
-    k.draft0 = dr.x;
-    k.drafts = dr.y;
-  }
-  for (int i = threadIdx.x; i < 16 * CT; i += 64 * kWaves) {
-    const int c = c0 + i, t = c >> a.rep_shift;
-    const bool live = t < dr.y;
-    sm.row[i] = live ? (dr.x + t) * a.num_q_heads + (h << a.rep_shift) + (c & ((1 << a.rep_shift) - 1)) : -1;
-    sm.mask[i] = live && piece_id == 0 ? a.masks[dr.x + t] : 0;
+  id -= a.prefix_blocks;
+  int u, rb;
+  locate(id, a.row_blocks, u, rb);
+  SeqUnit x;
+  const int c0 = rb * COLS;
+  if (!seq_unit(a, u, c0, threadIdx.x < 64, u_.order, x)) return;
+  for (int i = threadIdx.x; i < COLS; i += 64 * kWaves) {
+    sm.row[i] = column_row(a, x, c0 + i);
+    sm.mask[i] = column_mask(a, x, c0 + i);
   }
   __syncthreads();
-  unit<D, FP8, CT>(a, k, h, slot, sm);
+  rows_unit<D, FP8, RT>(a, x.k, x.h, x.slot, sm);
+}
+
+// Merges the partial results of every row:
+//   lse = ln sum_i exp(lse_i),  out = sum_i exp(lse_i - lse) o_i
+// over the row's parts that are not empty (lse_i = -inf), as one pass with a
+// running maximum. D / 4 lanes hold a row; rows in the order of the parts.
+template <int D>
+__global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
+  constexpr int LPR = D / 4, BATCH = 4;
+  const long long rows = (long long)a.num_drafts * a.num_q_heads;
+  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) / LPR;
+  if (i >= rows) return;
+  const int per_head = a.num_drafts << a.rep_shift;
+  const int h = (int)(i / per_head), c = (int)(i - (long long)h * per_head), t = c >> a.rep_shift;
+  const int n = t < a.draft_offs[a.num_seqs] ? min(a.token_parts[t], a.max_prefix_chunks + a.max_pieces) : 0;
+  if (n <= 0) return;  // behind the last sequence, or stored already
+  const int sub = threadIdx.x % LPR;
+  const float* lse = a.part_lse + i;
+  const f32x4_t* o = reinterpret_cast<const f32x4_t*>(a.part_o) + (size_t)i * LPR + sub;
+  float m = -INFINITY, w = 0.f;
+  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < n; k += BATCH) {
+    float l[BATCH];
+    f32x4_t x[BATCH];
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      l[b] = -INFINITY;
+      if (k + b < n) {
+        l[b] = lse[(size_t)(k + b) * rows];
+        x[b] = o[(size_t)(k + b) * rows * LPR];
+      }
+    }
+    float top = m;
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) top = fmaxf(top, l[b]);
+    const float f = m == top ? 1.f : fast_exp2((m - top) * kLog2e);
+    w *= f;
+    acc *= f;
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      if (l[b] == -INFINITY) continue;
+      const float e = l[b] == top ? 1.f : fast_exp2((l[b] - top) * kLog2e);
+      w += e;
+      acc += e * x[b];
+    }
+    m = top;
+  }
+  const float inv = w == 0.f ? 0.f : 1.f / w;
+  const size_t row = (size_t)t * a.num_q_heads + ((size_t)h << a.rep_shift) + (c & ((1 << a.rep_shift) - 1));
+  acc *= inv;
+  *reinterpret_cast<uint2*>(a.out + row * D + sub * 4) = make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));
+  if (a.lse != nullptr && sub == 0) a.lse[row] = w == 0.f ? -INFINITY : m + fast_log2(w) * kLn2;
 }
 
 template <int D, bool FP8>
-hipError_t by_tiles(const TreeArgs& a, int tiles, unsigned blocks, hipStream_t st) {
+hipError_t by_form(const TreeArgs& a, TreeForm form, unsigned blocks, hipStream_t st) {
   const dim3 grid(blocks), threads(64 * kWaves);
-  switch (tiles) {
-    case 1: tree_kernel<D, FP8, 1><<<grid, threads, 0, st>>>(a); break;
-    case 2: tree_kernel<D, FP8, 2><<<grid, threads, 0, st>>>(a); break;
-    case 4: tree_kernel<D, FP8, 4><<<grid, threads, 0, st>>>(a); break;
-    default: return hipErrorInvalidValue;
+  switch (form) {
+    case TreeForm::kSplit1: tree_split_kernel<D, FP8, 1><<<grid, threads, 0, st>>>(a); break;
+    case TreeForm::kSplit2: tree_split_kernel<D, FP8, 2><<<grid, threads, 0, st>>>(a); break;
+    case TreeForm::kSplit4: tree_split_kernel<D, FP8, 4><<<grid, threads, 0, st>>>(a); break;
+    case TreeForm::kRows: tree_rows_kernel<D, FP8, 2><<<grid, threads, 0, st>>>(a); break;
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_tree_attn(const TreeArgs& a, int head_dim, bool fp8, int tiles, long long blocks,
+hipError_t launch_tree_merge(const TreeArgs& a, int head_dim, hipStream_t stream) {
+  const long long threads = (long long)a.num_drafts * a.num_q_heads * (head_dim / 4), blocks = (threads + 255) / 256;
+  if (blocks <= 0) return hipSuccess;
+  if (blocks > kMaxBlocks256) return hipErrorInvalidValue;
+  if (head_dim == 128) tree_merge_kernel<128><<<(unsigned)blocks, 256, 0, stream>>>(a);
+  else tree_merge_kernel<64><<<(unsigned)blocks, 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_tree_attn(const TreeArgs& a, int head_dim, bool fp8, TreeForm form, long long blocks,
                             hipStream_t stream) {
   if (blocks <= 0) return hipSuccess;
-  if (blocks >= (1ll << 31)) return hipErrorInvalidValue;
+  if (blocks > kMaxBlocks256) return hipErrorInvalidValue;
   const unsigned n = (unsigned)blocks;
-  if (head_dim == 128) return fp8 ? by_tiles<128, true>(a, tiles, n, stream) : by_tiles<128, false>(a, tiles, n, stream);
-  if (head_dim == 64) return fp8 ? by_tiles<64, true>(a, tiles, n, stream) : by_tiles<64, false>(a, tiles, n, stream);
+  if (head_dim == 128) return fp8 ? by_form<128, true>(a, form, n, stream) : by_form<128, false>(a, form, n, stream);
+  if (head_dim == 64) return fp8 ? by_form<64, true>(a, form, n, stream) : by_form<64, false>(a, form, n, stream);
   return hipErrorInvalidValue;
 }
 

@@ -77,6 +77,32 @@ def test_more_group_rows_than_row_blocks_in_the_grid(dtype):
     check_tree(wl, [16] * 40, 4, f"tree one group of many {dtype}")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("hq,hkv,d,most", [(4, 2, 128, 3), (2, 2, 64, 3), (8, 1, 64, 40), (8, 1, 128, 40), (16, 4, 64, 2)])
+def test_long_prefixes_of_many_members(hq, hkv, d, most, dtype):
+    """Prefixes that pay to be read once for all members: units of their own, of several chunks, for row counts on
+    both sides of a workgroup's, with members in any order, some without drafts, another group without a prefix."""
+    rng = np.random.default_rng(hq + most)
+    counts = rng.integers(0, 3, 60)
+    counts[7] = most
+    groups = np.where(rng.random(60) < 0.9, 1, 0)
+    wl = _wl(hq, hkv, d, dtype, groups, [0, 3000], rng.integers(0, 120, 60), seed=5, max_resp_pages=WIDE)
+    check_tree(wl, counts, 6, f"tree long prefix {hq} {hkv} {d} {most} {dtype}", max_drafts=most)
+    wl = _wl(hq, hkv, d, dtype, groups, [33, 1601], rng.integers(0, 120, 60), seed=5)
+    check_tree(wl, counts, 6, f"tree long prefix {hq} {hkv} {d} {most} {dtype}, short table", max_drafts=most)
+
+
+def test_many_sequences_of_all_lengths():
+    """More units than a launch orders at once by length, with ties, empty ones and one that is far the longest."""
+    rng = np.random.default_rng(2)
+    L = rng.integers(0, 200, 700)
+    L[::7], L[300], L[:5] = 64, 6000, 0
+    wl = _wl(2, 2, 64, "bf16", np.arange(700) % 5, [10, 0, 40, 3, 100], L, seed=5)
+    check_tree(wl, 1 + np.arange(700) % 2, 6, "tree 700 lengths", max_drafts=2)
+    wl = _wl(1, 1, 64, "fp8", np.arange(1100) % 5, [10, 0, 40, 3, 100], rng.integers(0, 90, 1100), seed=5)
+    check_tree(wl, np.ones(1100, int), 6, "tree 1100 sequences", max_drafts=1)
+
+
 @pytest.mark.parametrize("width", [None, WIDE])
 @pytest.mark.parametrize("dtype", ["bf16", "fp8"])
 def test_masks_of_any_kind(dtype, width):
