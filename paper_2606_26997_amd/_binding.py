@@ -173,7 +173,8 @@ def _ptr(t) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is None:
         # The raw handle of torch's current stream: a Stream object costs 2.7 us, more than a launch.
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if torch.cuda.is_available() else None
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) \
+            if torch.cuda.is_initialized() or torch.cuda.is_available() else None
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

@@ -684,9 +684,8 @@ rp_status rp_kv_write_slots(const rp_paged_kv* kv, const int32_t* slot_map, int3
   if (st != RP_OK) return st;
   if (num_tokens < 0 || num_src < 0) return fail(RP_ERR_INVALID_ARG, "num_tokens/num_src must be >= 0");
   if (kv->num_pages >= (1 << 27)) return fail(RP_ERR_UNSUPPORTED, "slots of %d pages pass 32 bits", kv->num_pages);
-  // Blocks of the launch: pieces of 16 bytes, or (bits of the list, kv-head).
-  if ((long long)num_tokens * kv->num_kv_heads * kv->head_dim >= (1ll << 40) ||
-      (long long)num_tokens * kv->num_kv_heads >= (1ll << 30))
+  // A launch has fewer than 2^32 threads: 2 D / 8 for each row of bf16.
+  if ((long long)num_tokens * kv->num_kv_heads * (kv->head_dim / 4) >= (1ll << 32) - 256)
     return fail(RP_ERR_UNSUPPORTED, "too many rows for one call");
   if (num_tokens == 0 || num_src == 0) return RP_OK;
   if (slot_map == nullptr || !aligned(slot_map, 4) || !aligned(src_rows, 4))
@@ -706,7 +705,13 @@ rp_status rp_kv_write_slots(const rp_paged_kv* kv, const int32_t* slot_map, int3
   a.src_rows = src_rows;
   a.k_new = k_new;
   a.v_new = v_new;
-  a.chunk = 16;
+  // fp8: few entries per wave while there are few, so that no wave does many
+  // runs one after the other, and 16 where the waves that begin no run would
+  // count. us at 1, 4, 8, 16 entries (Hkv 8, d 128): 16 rows alone 8.2, 8.8, 13,
+  // 21; 1024 alone 11.8, 13.3, 16, 24; 1024 runs of 8 36.8, 27.8, 20.4, 22.2; 64
+  // prompts of 1024 234, 116, 98, 85.
+  const long long waves = 2ll * num_tokens * kv->num_kv_heads;
+  a.chunk = (int)std::min(std::max((waves + 12287) / 12288, 1ll), 16ll);
   hipError_t e = rp::launch_write_slots(a, kv->head_dim, rp::enum_bits(kv->kv_dtype) == RP_KV_FP8_E4M3, stream);
   return e == hipSuccess ? RP_OK : hip_fail(e, "slot write kernel launch");
 }
@@ -748,7 +753,7 @@ rp_status rp_page_tables_resize(const rp_page_tables* t, const int32_t* old_lens
   a.slot_offs = slot_offs;
   a.slot_map = slot_map;
   a.status = status;
-  hipError_t e = rp::launch_page_tables(a, 1, stream);
+  hipError_t e = rp::launch_page_tables(a, stream);
   return e == hipSuccess ? RP_OK : hip_fail(e, "page table kernel launch");
 }
 

@@ -254,8 +254,8 @@ hipError_t launch_tree_merge(const TreeArgs& a, int head_dim, hipStream_t stream
 hipError_t launch_tree_attn(const TreeArgs& a, int head_dim, bool fp8, TreeForm form, long long blocks,
                             hipStream_t stream);
 hipError_t launch_write_slots(const WriteArgs& a, int head_dim, bool fp8, hipStream_t stream);
-// blocks: workgroups (1: one launch, else two).
-hipError_t launch_page_tables(const TableArgs& a, int blocks, hipStream_t stream);
+// One launch, or two where much moves.
+hipError_t launch_page_tables(const TableArgs& a, hipStream_t stream);
 hipError_t launch_append(const AppendArgs& a, int head_dim, bool fp8, hipStream_t stream);
 hipError_t launch_prefill_kv_write(const PrefillArgs& a, int head_dim, bool fp8, hipStream_t stream);
 hipError_t launch_prefill_attn(const PrefillArgs& a, int head_dim, int n_rep, hipStream_t stream);

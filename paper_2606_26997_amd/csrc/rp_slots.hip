@@ -9,6 +9,8 @@
 // rp_page_tables_resize: two exclusive prefix sums over the sequences (pages
 // given back, pages taken) say where each page of a block table goes on, or
 // comes from, the stack of free pages.
+#include <algorithm>
+
 #include "rp_device.h"
 #include "rp_internal.h"
 
@@ -122,83 +124,89 @@ __global__ __launch_bounds__(64) void write_fp8_kernel(const WriteArgs a) {
 
 // ---- page tables --------------------------------------------------------------
 
-constexpr int kTableThreads = 1024;
-
 // Exclusive prefix sums over the sequences, the same in every workgroup.
 struct Sums {
   int back[kTableMaxSeqs + 1];   // pages given back
   int take[kTableMaxSeqs + 1];   // pages taken
   int fresh[kTableMaxSeqs + 1];  // new tokens
-  long long part[3][kTableThreads / 64];
+  int old_len[kTableMaxSeqs], new_len[kTableMaxSeqs];
+  long long part[3][16];
   int bad, count;
 };
 
-__device__ inline void page_counts(int old_len, int new_len, int& back, int& take, int& fresh) {
-  const int have = (old_len + kPage - 1) / kPage, want = (new_len + kPage - 1) / kPage;
-  back = max(have - want, 0);
-  take = max(want - have, 0);
-  fresh = max(new_len - old_len, 0);
+__device__ inline int pages_of(int len) { return (len + kPage - 1) / kPage; }
+
+// Inclusive sum over the lanes of a wave.
+__device__ inline int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);  // lane - 1, - 2, - 4, - 8 of a row of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, true);  // the row before's last lane, into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, true);  // lane 31, into rows 2 and 3
+  return x;
+}
+__device__ inline long long wave_scan(long long x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long y = __shfl_up(x, o);
+    x += lane >= o ? y : 0;
+  }
+  return x;
 }
 
-// Fills the sums and returns the call's status.
+// Fills the sums and returns the call's status. Sum: the type that holds any
+// sum of new tokens that the table could.
+template <class Sum>
 __device__ int sum_up(const TableArgs& a, Sums& m, long long (&total)[3]) {
-  constexpr int PER = kTableMaxSeqs / kTableThreads;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
   if (tid == 0) {
     m.bad = 0;
     m.count = *a.free_count;
   }
-  __syncthreads();
-  const int per = cdiv(a.num_seqs, kTableThreads);  // sequences per thread, consecutive ones
+  const int per = cdiv(a.num_seqs, (int)blockDim.x), s0 = tid * per;  // consecutive sequences of a thread
   const int cap = a.max_pages * kPage;
-  int v[PER][3];
-  long long x[3] = {0, 0, 0};
+  Sum x[3] = {0, 0, 0};
   bool bad = false;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int s = tid * per + i;
-    v[i][0] = v[i][1] = v[i][2] = 0;
-    if (i < per && s < a.num_seqs) {
-      const int o = a.old_lens[s], n = a.new_lens[s];
-      const bool fits = o >= 0 && o <= cap && n >= 0 && n <= cap;
-      bad = bad || !fits;
-      if (fits) page_counts(o, n, v[i][0], v[i][1], v[i][2]);
-    }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) x[k] += v[i][k];
+  for (int i = 0; i < per && s0 + i < a.num_seqs; ++i) {
+    const int s = s0 + i, o = a.old_lens[s], n = a.new_lens[s];
+    const bool fits = o >= 0 && o <= cap && n >= 0 && n <= cap;
+    bad = bad || !fits;
+    m.old_len[s] = fits ? o : 0;
+    m.new_len[s] = fits ? n : 0;
+    if (!fits) continue;
+    const int d = pages_of(n) - pages_of(o);
+    x[0] += max(-d, 0);
+    x[1] += max(d, 0);
+    x[2] += max(n - o, 0);
   }
-  long long run[3];
+  Sum run[3];
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
-    long long y = x[k];
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const long long z = __shfl_up(y, o);
-      y += lane >= o ? z : 0;
-    }
+    const Sum y = wave_scan(x[k]);
     if (lane == 63) m.part[k][wave] = y;
     run[k] = y - x[k];
   }
-  if (bad) m.bad = 1;
   __syncthreads();
+  if (bad) m.bad = 1;
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
     total[k] = 0;
-    for (int w = 0; w < kTableThreads / 64; ++w) {
-      run[k] += w < wave ? m.part[k][w] : 0;
+    for (int w = 0; w < waves; ++w) {
+      run[k] += w < wave ? (Sum)m.part[k][w] : 0;
       total[k] += m.part[k][w];
     }
   }
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int s = tid * per + i;
-    if (i < per && s < a.num_seqs) {
-      m.back[s] = (int)run[0];
-      m.take[s] = (int)run[1];
-      m.fresh[s] = (int)run[2];
-    }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) run[k] += v[i][k];
+  for (int i = 0; i < per && s0 + i < a.num_seqs; ++i) {
+    const int s = s0 + i, o = m.old_len[s], n = m.new_len[s], d = pages_of(n) - pages_of(o);
+    m.back[s] = (int)run[0];
+    m.take[s] = (int)run[1];
+    m.fresh[s] = (int)run[2];
+    run[0] += max(-d, 0);
+    run[1] += max(d, 0);
+    run[2] += max(n - o, 0);
   }
   if (tid == 0) {
     m.back[a.num_seqs] = (int)total[0];
@@ -225,51 +233,74 @@ __device__ inline int owner(const int* sums, int n, int rank) {
   return lo;
 }
 
-__device__ inline int first_page(int len) { return (len + kPage - 1) / kPage; }
+// Table entry of the page given back, or taken, with rank r.
+__device__ inline int* back_entry(const TableArgs& a, const Sums& m, int r) {
+  const int s = owner(m.back, a.num_seqs, r);
+  return a.block_table + (size_t)s * a.max_pages + pages_of(m.new_len[s]) + (r - m.back[s]);
+}
+__device__ inline int* take_entry(const TableArgs& a, const Sums& m, int r) {
+  const int s = owner(m.take, a.num_seqs, r);
+  return a.block_table + (size_t)s * a.max_pages + pages_of(m.old_len[s]) + (r - m.take[s]);
+}
 
 // Pages of rank `item`, `item` + `step` ...: given back, then taken. The page
 // given back with rank f goes to place top - 1 - f of the stack, and the page
 // taken with rank o comes from place top - 1 - o: for o below the number given
 // back that is the page of rank o among those, which whoever gives it back
-// hands over, so nothing that this call writes is read by it.
-__device__ void move_pages(const TableArgs& a, const Sums& m, int item, int step) {
-  const int S = a.num_seqs, F = m.back[S], N = m.take[S];
-  const long long top = (long long)m.count + F;
-  for (int f = item; f < F; f += step) {
-    const int s = owner(m.back, S, f);
-    int* at = a.block_table + (size_t)s * a.max_pages + first_page(a.new_lens[s]) + (f - m.back[s]);
-    const int page = *at;
-    *at = -1;
-    a.free_pages[top - 1 - f] = page;
-    if (f < N) {
-      const int t = owner(m.take, S, f);
-      a.block_table[(size_t)t * a.max_pages + first_page(a.old_lens[t]) + (f - m.take[t])] = page;
-    }
+// hands over, so nothing that this call writes is read by it. between(): after
+// the first of them have been read, before anything is written.
+template <class F>
+__device__ void move_pages(const TableArgs& a, const Sums& m, int item, int step, F between) {
+  const int F_ = m.back[a.num_seqs], N = m.take[a.num_seqs];
+  const long long top = (long long)m.count + F_;
+  const int f0 = item, o0 = F_ + item;
+  int *from = nullptr, *to = nullptr, given = 0, taken = 0;
+  if (f0 < F_) {
+    from = back_entry(a, m, f0);
+    given = *from;
   }
-  for (int o = F + item; o < N; o += step) {
-    const int s = owner(m.take, S, o);
-    a.block_table[(size_t)s * a.max_pages + first_page(a.old_lens[s]) + (o - m.take[s])] = a.free_pages[top - 1 - o];
+  if (o0 < N) {
+    to = take_entry(a, m, o0);
+    taken = a.free_pages[top - 1 - o0];
+  }
+  between();
+  for (int f = f0; f < F_; f += step) {
+    if (f != f0) {
+      from = back_entry(a, m, f);
+      given = *from;
+    }
+    *from = -1;
+    a.free_pages[top - 1 - f] = given;
+    if (f < N) *take_entry(a, m, f) = given;
+  }
+  for (int o = o0; o < N; o += step) {
+    if (o != o0) {
+      to = take_entry(a, m, o);
+      taken = a.free_pages[top - 1 - o];
+    }
+    *to = taken;
   }
 }
 
-__device__ void write_slots(const TableArgs& a, const int* fresh, int status, long long item, long long step) {
-  const int total = status == RP_TABLES_OK ? fresh[a.num_seqs] : 0;
-  for (long long t = item; t < a.max_slots; t += step) {
+// Slots t0, t0 + step ... of the new tokens; page(s, p): page p of sequence s.
+template <class F>
+__device__ void write_slots(const TableArgs& a, const int* fresh, const int* old_len, int total, long long t0,
+                            long long step, F page) {
+  for (long long t = t0; t < a.max_slots; t += step) {
     int slot = -1;
     if (t < total) {
       const int s = owner(fresh, a.num_seqs, (int)t);
-      const int pos = a.old_lens[s] + ((int)t - fresh[s]);
-      slot = a.block_table[(size_t)s * a.max_pages + pos / kPage] * kPage + pos % kPage;
+      const int pos = old_len[s] + ((int)t - fresh[s]);
+      slot = page(s, pos / kPage) * kPage + pos % kPage;
     }
     a.slot_map[t] = slot;
   }
 }
 
 __device__ void tell(const TableArgs& a, const Sums& m, int status, const long long (&total)[3]) {
-  const int tid = threadIdx.x;
   if (a.slot_offs != nullptr)
-    for (int s = tid; s <= a.num_seqs; s += kTableThreads) a.slot_offs[s] = status == RP_TABLES_OK ? m.fresh[s] : 0;
-  if (tid == 0) {
+    for (int s = threadIdx.x; s <= a.num_seqs; s += blockDim.x) a.slot_offs[s] = status == RP_TABLES_OK ? m.fresh[s] : 0;
+  if (threadIdx.x == 0) {
     a.status[0] = status;
     a.status[1] = (int)total[1];
     a.status[2] = (int)total[0];
@@ -277,39 +308,64 @@ __device__ void tell(const TableArgs& a, const Sums& m, int status, const long l
   }
 }
 
-// Everything in one workgroup.
-__global__ __launch_bounds__(kTableThreads) void tables_one_kernel(const TableArgs a) {
+// Everything in one workgroup: the slots from what the tables hold before, with
+// new pages by their rank, in the shadow of the first moves' loads.
+template <class Sum>
+__global__ __launch_bounds__(1024) void tables_one_kernel(const TableArgs a) {
   __shared__ Sums m;
   long long total[3];
-  const int status = sum_up(a, m, total);
-  tell(a, m, status, total);
-  if (status == RP_TABLES_OK) {
-    move_pages(a, m, threadIdx.x, kTableThreads);
+  const int status = sum_up<Sum>(a, m, total);
+  const bool done = status == RP_TABLES_OK;
+  const auto slots = [&]() {
+    if (a.slot_map != nullptr) {
+      const long long top = m.count + total[0];
+      write_slots(a, m.fresh, m.old_len, done ? (int)total[2] : 0, threadIdx.x, blockDim.x, [&](int s, int p) {
+        const int rank = m.take[s] + p - pages_of(m.old_len[s]);
+        if (p < pages_of(m.old_len[s])) return a.block_table[(size_t)s * a.max_pages + p];
+        return rank < total[0] ? *back_entry(a, m, rank) : a.free_pages[top - 1 - rank];
+      });
+    }
+    __syncthreads();  // every read of what was there is done
+  };
+  if (done) {
+    move_pages(a, m, threadIdx.x, blockDim.x, slots);
     if (threadIdx.x == 0) *a.free_count = (int)(m.count + total[0] - total[1]);
+  } else {
+    slots();
   }
-  __syncthreads();  // the tables are written
-  if (a.slot_map != nullptr) write_slots(a, m.fresh, status, threadIdx.x, kTableThreads);
+  tell(a, m, status, total);
 }
 
 // The same in two launches of many workgroups: pages, then slots and the count
 // of free pages, which every workgroup of the first one reads.
-__global__ __launch_bounds__(kTableThreads) void tables_pages_kernel(const TableArgs a) {
+template <class Sum>
+__global__ __launch_bounds__(1024) void tables_pages_kernel(const TableArgs a) {
   __shared__ Sums m;
   long long total[3];
-  const int status = sum_up(a, m, total);
+  const int status = sum_up<Sum>(a, m, total);
   if (blockIdx.x == 0) tell(a, m, status, total);
   if (status == RP_TABLES_OK)
-    move_pages(a, m, blockIdx.x * kTableThreads + threadIdx.x, gridDim.x * kTableThreads);
+    move_pages(a, m, blockIdx.x * blockDim.x + threadIdx.x, gridDim.x * blockDim.x, [] {});
 }
-__global__ __launch_bounds__(kTableThreads) void tables_slots_kernel(const TableArgs a) {
-  __shared__ int fresh[kTableMaxSeqs + 1];
+__global__ __launch_bounds__(1024) void tables_slots_kernel(const TableArgs a) {
+  __shared__ int fresh[kTableMaxSeqs + 1], old_len[kTableMaxSeqs];
   const int status = a.status[0];
   if (blockIdx.x == 0 && threadIdx.x == 0 && status == RP_TABLES_OK) *a.free_count += a.status[2] - a.status[1];
   if (a.slot_map == nullptr) return;
-  for (int s = threadIdx.x; s <= a.num_seqs; s += kTableThreads) fresh[s] = a.slot_offs[s];
+  for (int s = threadIdx.x; s <= a.num_seqs; s += blockDim.x) {
+    fresh[s] = a.slot_offs[s];
+    if (s < a.num_seqs) old_len[s] = a.old_lens[s];
+  }
   __syncthreads();
-  write_slots(a, fresh, status, (long long)blockIdx.x * kTableThreads + threadIdx.x,
-              (long long)gridDim.x * kTableThreads);
+  write_slots(a, fresh, old_len, status == RP_TABLES_OK ? fresh[a.num_seqs] : 0,
+              (long long)blockIdx.x * blockDim.x + threadIdx.x, (long long)gridDim.x * blockDim.x,
+              [&](int s, int p) { return a.block_table[(size_t)s * a.max_pages + p]; });
+}
+
+template <class Sum>
+void tables_launch(const TableArgs& a, int blocks, int threads, hipStream_t stream) {
+  if (blocks == 1) tables_one_kernel<Sum><<<1, threads, 0, stream>>>(a);
+  else tables_pages_kernel<Sum><<<blocks, threads, 0, stream>>>(a);
 }
 
 }  // namespace
@@ -319,29 +375,34 @@ hipError_t launch_write_slots(const WriteArgs& a, int head_dim, bool fp8, hipStr
   if (head_dim != 128 && head_dim != 64) return hipErrorInvalidValue;
   if (fp8) {
     const long long blocks = ((long long)a.num_tokens + a.chunk - 1) / a.chunk * 2 * a.num_kv_heads;
-    if (a.chunk < 1 || a.chunk > 48 || blocks >= (1ll << 31)) return hipErrorInvalidValue;
+    if (a.chunk < 1 || a.chunk > 48 || blocks > 4 * kMaxBlocks256) return hipErrorInvalidValue;
     if (head_dim == 128) write_fp8_kernel<128><<<(unsigned)blocks, 64, 0, stream>>>(a);
     else write_fp8_kernel<64><<<(unsigned)blocks, 64, 0, stream>>>(a);
   } else {
     const long long pieces = (long long)a.num_tokens * 2 * a.num_kv_heads * (head_dim / 8);
     const long long blocks = (pieces + kWriteThreads - 1) / kWriteThreads;
-    if (blocks >= (1ll << 31)) return hipErrorInvalidValue;
+    if (blocks > kMaxBlocks256) return hipErrorInvalidValue;
     if (head_dim == 128) write_bf16_kernel<128><<<(unsigned)blocks, kWriteThreads, 0, stream>>>(a);
     else write_bf16_kernel<64><<<(unsigned)blocks, kWriteThreads, 0, stream>>>(a);
   }
   return hipGetLastError();
 }
 
-hipError_t launch_page_tables(const TableArgs& a, int blocks, hipStream_t stream) {
-  if (a.num_seqs > kTableMaxSeqs || blocks < 1) return hipErrorInvalidValue;
-  if (blocks == 1) {
-    tables_one_kernel<<<1, kTableThreads, 0, stream>>>(a);
-    return hipGetLastError();
-  }
-  tables_pages_kernel<<<blocks, kTableThreads, 0, stream>>>(a);
+hipError_t launch_page_tables(const TableArgs& a, hipStream_t stream) {
+  if (a.num_seqs > kTableMaxSeqs) return hipErrorInvalidValue;
+  // One workgroup where little can move, by the table and the slots: it takes
+  // about 1 us for 1000 pages or slots, and the second launch about 5 us (16
+  // sequences x 377 pages, 136 new tokens: one launch 3.8 us, two 8.9; 1024 x
+  // 129, a quarter of them ending: one launch 150 us, two 14.4).
+  const long long entries = (long long)a.num_seqs * a.max_pages, work = std::max<long long>(a.max_slots, entries);
+  const int blocks = work <= 8192 ? 1 : (int)std::min(std::max(2ll, work / 1024), 256ll);
+  const int threads = blocks > 1 || a.max_slots > 1024 || a.num_seqs > 256 ? 1024 : 256;
+  const bool wide = entries * kPage >= (1ll << 31);
+  if (wide) tables_launch<long long>(a, blocks, threads, stream);
+  else tables_launch<int>(a, blocks, threads, stream);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  tables_slots_kernel<<<blocks, kTableThreads, 0, stream>>>(a);
+  if (e != hipSuccess || blocks == 1) return e;
+  tables_slots_kernel<<<blocks, threads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
