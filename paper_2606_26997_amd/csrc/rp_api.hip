@@ -365,8 +365,8 @@ constexpr int kTreeLeastPages = 32;
 // read, at about 1.2 TB/s, and the second launch where nothing else needs it.
 struct TreePlan {
   rp::TreeForm form;
-  bool share, ordered;
-  int row_blocks, chunk, max_pc, piece, max_pieces, ppr, repeats;
+  bool share;
+  int longest_first, row_blocks, chunk, max_pc, piece, max_pieces, ppr, repeats;
   long long prefix_blocks, blocks;
   size_t parts, part_o, part_lse, total;
 };
@@ -419,7 +419,14 @@ bool tree_plan(const Shape& sh, const rp_draft_tree* t, TreePlan* p) {
   p->max_pieces = rp::cdiv(pages, p->piece);
   p->ppr = p->max_pc + p->max_pieces;
   if (p->ppr == 1) p->ppr = 0;  // every result is final
-  p->ordered = base > kTreeUnits && sh.S <= rp::kTreeOrderSeqs;
+  // The longest first; where one unit per sequence and kv-head fills the chip
+  // once, two to a compute unit, the second one there has the shorter the
+  // longer the first is (64 sequences of U[0, 7600] tokens, 8 kv-heads: as they
+  // come 200 us, so 165; 32 of 1024 + U[0, 2048] with 64 drafts 135 and 119).
+  p->longest_first = 0;
+  if (sh.S <= rp::kTreeOrderSeqs && base > kTreeUnits) p->longest_first = sh.S;
+  if (sh.S <= rp::kTreeOrderSeqs && base <= kTreeUnits && base > kTreeUnits / 2 && p->max_pieces == 1 && pages >= 64)
+    p->longest_first = (int)((sh.S * (kTreeUnits / 2) + base - 1) / base);
   const auto grid = [](long long units, long long repeats) { return (units + 7) / 8 * 8 * repeats; };
   p->prefix_blocks = p->share ? grid((long long)sh.G * p->max_pc * sh.Hkv, p->repeats) : 0;
   p->blocks = p->prefix_blocks + grid(pairs * p->max_pieces, p->row_blocks);
@@ -662,7 +669,7 @@ rp_status rp_group_tree_attn(const rp_paged_kv* kv, const rp_group_layout* l, co
     a.part_lse = reinterpret_cast<float*>(b + p.part_lse);
   }
   a.share = p.share ? 1 : 0;
-  a.ordered = p.ordered ? 1 : 0;
+  a.longest_first = p.longest_first;
   a.prefix_chunk = p.chunk;
   a.max_prefix_chunks = p.max_pc;
   a.prefix_repeats = p.repeats;

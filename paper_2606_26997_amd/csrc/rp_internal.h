@@ -189,7 +189,7 @@ struct TreeArgs {
   int* token_parts;                  // [T] partial results of each row of a token, 0: it is stored already
   // How the launch is divided.
   int share;                         // prefixes are units of their own, for all members at once
-  int ordered;                       // sequences by decreasing length
+  int longest_first;                 // so many sequences by decreasing length, the others by increasing; 0: as they are
   int prefix_chunk, max_prefix_chunks, prefix_repeats, prefix_blocks;
   int piece_pages, max_pieces, row_blocks;
 };

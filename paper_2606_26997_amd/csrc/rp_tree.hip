@@ -43,6 +43,14 @@ __device__ inline u32x4_t decode8(uint32_t w0, uint32_t w1) {
   return u32x4_t{decode2<false>(w0), decode2<true>(w0), decode2<false>(w1), decode2<true>(w1)};
 }
 
+// 16 codes, decoded, to 32 bytes of LDS. Neighbouring lanes' pieces follow each
+// other there, so with the halves in one order half of the banks would get all
+// of a write: odd lanes write their second half first.
+__device__ inline void store_decoded(u32x4_t* dst, const u32x4_t& w, int odd) {
+  dst[odd] = decode8(odd ? w.z : w.x, odd ? w.w : w.y);
+  dst[1 - odd] = decode8(odd ? w.x : w.z, odd ? w.y : w.w);
+}
+
 template <int D, bool FP8, int CT>
 struct Shape {
   static constexpr int EB = FP8 ? 1 : 2;                  // bytes per cached element
@@ -55,13 +63,14 @@ struct Shape {
   static constexpr int PAGES = 4 / LOADS / (FP8 && CT == 4 ? 2 : 1);
   static constexpr int DT = D / 16;
   static constexpr int PITCH = D + 16;                    // staged V row: a transposing read meets no bank twice
-  static constexpr int STAGE = PAGES * kPage * PITCH;     // per wave, bf16 elements
+  static constexpr bool PAIR = PAGES == 1 && CT == 4;     // P V of two one-page steps at once
+  static constexpr int STAGE = (PAIR ? 2 : PAGES) * kPage * PITCH;  // per wave, bf16 elements
   static constexpr int COLS = 16 * CT;
   static constexpr int OPITCH = D + 4;                    // merged output row, floats
   // The query operands of four tiles of 128-wide heads take 64 registers, too
   // many beside the 128 of the output: they stay in LDS.
   static constexpr bool QLDS = CT * D >= 512;
-  static constexpr int QPITCH = D + 8;
+  static constexpr int QPITCH = D + 16;
   static constexpr int LOOP_BYTES = (kWaves * STAGE + (QLDS ? COLS * QPITCH : 0)) * 2;
   static constexpr int MERGE_BYTES = kWaves * 16 * OPITCH * 4;
   static constexpr int BYTES = LOOP_BYTES > MERGE_BYTES ? LOOP_BYTES : MERGE_BYTES;
@@ -111,16 +120,17 @@ struct State {
 // less the running maximum, -inf where hidden) become rounded probabilities,
 // times the blocks' V scales vs where SCALED. The maximum moves, and the
 // accumulator is rescaled, only when a score exceeds it by more than the
-// headroom. EXACT: normalised by the exact sum alone.
-template <int D, int T, int N, bool SCALED, bool EXACT>
+// headroom; before() then comes first. EXACT: normalised by the exact sum alone.
+template <int D, int T, int N, bool SCALED, bool EXACT, class Before>
 __device__ __forceinline__ void softmax_step(State<D, T>& st, int t, f32x4_t (&x)[N], const float (&vs)[N],
-                                             bf16x4_t (&pop)[N]) {
+                                             bf16x4_t (&pop)[N], Before before) {
   float mx = -INFINITY;
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) mx = fmaxf(mx, x[i][e]);
   if (__any(mx > st.thr[t])) {
+    before();
     mx = max_xor16_32(mx);
     const float up = mx > st.thr[t] ? mx : 0.f;
     const float alpha = st.thr[t] == -INFINITY ? 0.f : fast_exp2(-up);  // nothing yet: 0 times it
@@ -226,7 +236,7 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
   }
   const auto qop = [&](int t, int j, int hh) __attribute__((always_inline)) {
     if constexpr (G::QLDS)
-      return *reinterpret_cast<const bf16x8_t*>(ql + (t * 16 + r16) * G::QPITCH + (quad + 4 * j) * EPL + hh * 8);
+      return *reinterpret_cast<const bf16x8_t*>(ql + (t * 16 + r16) * G::QPITCH + (j * (EPL / 8) + hh) * 32 + quad * 8);
     else
       return qreg[t][j][hh];
   };
@@ -285,7 +295,9 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
     };
     load_k(0);
     load_v(0);
-    for (int p = 0; p < npg; p += PAGES) {
+    // Scores, staged V (page `at` of the staging area) and probabilities of one
+    // step; before(t): see softmax_step.
+    const auto scores = [&](int p, int at, bf16x4_t (&pop)[CT][PAGES], auto before) __attribute__((always_inline)) {
       f32x4_t s[CT][PAGES];
 #pragma unroll
       for (int i = 0; i < PAGES; ++i) {
@@ -317,15 +329,11 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
           const int e0 = (j * 64 + lane) * EPL, tok = e0 / D, col = e0 % D;
-          u32x4_t* dst = reinterpret_cast<u32x4_t*>(vt + (i * kPage + tok) * PITCH + col);
+          u32x4_t* dst = reinterpret_cast<u32x4_t*>(vt + ((at + i) * kPage + tok) * PITCH + col);
           u32x4_t w = vx[i][j];
           if (ragged) w = tok < nv ? w : u32x4_t{0, 0, 0, 0};  // padding rows may hold anything
-          if constexpr (!FP8) {
-            dst[0] = w;
-          } else {
-            dst[0] = decode8(w.x, w.y);
-            dst[1] = decode8(w.z, w.w);
-          }
+          if constexpr (!FP8) dst[0] = w;
+          else store_decoded(dst, w, lane & 1);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -351,36 +359,76 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
             for (int e = 0; e < 4; ++e) s[t][i][e] = quad * 4 + e < nv ? s[t][i][e] : -INFINITY;
         }
       }
-      bf16x4_t pop[CT][PAGES];
 #pragma unroll
-      for (int t = 0; t < CT; ++t) softmax_step<D, CT, PAGES, FP8, FP8>(st, t, s[t], vs, pop[t]);
-
+      for (int t = 0; t < CT; ++t)
+        softmax_step<D, CT, PAGES, FP8, FP8>(st, t, s[t], vs, pop[t], [&] { before(t); });
       wave_lds_sync();  // the staged V is visible to the whole wave
-      if constexpr (PAGES == 1) {
+    };
+    // O^T += V^T P^T of one page, of tile t; of two pages, all tiles.
+    const auto add_page = [&](int at, int t, const bf16x4_t& pop) __attribute__((always_inline)) {
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const bf16x4_t v0 = lds_read_tr(vtr + dt * 16);
+      for (int dt = 0; dt < DT; ++dt)
+        st.o[t][dt] = mfma16x16x16(lds_read_tr(vtr + at * kPage * PITCH + dt * 16), pop, st.o[t][dt]);
+    };
+    const auto add_two = [&](int at, const bf16x4_t (&x)[CT], const bf16x4_t (&y)[CT]) __attribute__((always_inline)) {
 #pragma unroll
-          for (int t = 0; t < CT; ++t) st.o[t][dt] = mfma16x16x16(v0, pop[t][0], st.o[t][dt]);
-        }
-      } else {
+      for (int dt = 0; dt < DT; ++dt) {
+        const bf16x4_t v0 = lds_read_tr(vtr + at * kPage * PITCH + dt * 16);
+        const bf16x4_t v1 = lds_read_tr(vtr + (at + 1) * kPage * PITCH + dt * 16);
+        const bf16x8_t vo = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-        for (int i = 0; i < PAGES; i += 2)
+        for (int t = 0; t < CT; ++t)
+          st.o[t][dt] = mfma16x16x32(vo, __builtin_shufflevector(x[t], y[t], 0, 1, 2, 3, 4, 5, 6, 7), st.o[t][dt]);
+      }
+    };
+    const auto nothing = [](int) {};
+    if constexpr (G::PAIR) {
+      // The products with V take two pages' probabilities at once, at twice the
+      // rate. A maximum that moves in between first adds the first page's.
+      bf16x4_t first[CT][1], second[CT][1];
+      int p = 0;
+      for (; p + 1 < npg; p += 2) {
+        scores(p, 0, first, nothing);
+        scores(p + 1, 1, second, [&](int t) __attribute__((always_inline)) {
+          add_page(0, t, first[t][0]);
+          first[t][0] = __builtin_bit_cast(bf16x4_t, make_uint2(0, 0));
+        });
+        bf16x4_t x[CT], y[CT];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) x[t] = first[t][0], y[t] = second[t][0];
+        add_two(0, x, y);
+      }
+      if (p < npg) {
+        scores(p, 0, first, nothing);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) add_page(0, t, first[t][0]);
+      }
+    } else {
+      for (int p = 0; p < npg; p += PAGES) {
+        bf16x4_t pop[CT][PAGES];
+        scores(p, 0, pop, nothing);
+        if constexpr (PAGES == 1) {
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) {
-            const bf16x4_t v0 = lds_read_tr(vtr + i * kPage * PITCH + dt * 16);
-            const bf16x4_t v1 = lds_read_tr(vtr + (i + 1) * kPage * PITCH + dt * 16);
-            const bf16x8_t vo = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+            const bf16x4_t v0 = lds_read_tr(vtr + dt * 16);
 #pragma unroll
-            for (int t = 0; t < CT; ++t)
-              st.o[t][dt] = mfma16x16x32(
-                  vo, __builtin_shufflevector(pop[t][i], pop[t][i + 1], 0, 1, 2, 3, 4, 5, 6, 7), st.o[t][dt]);
+            for (int t = 0; t < CT; ++t) st.o[t][dt] = mfma16x16x16(v0, pop[t][0], st.o[t][dt]);
           }
+        } else {
+#pragma unroll
+          for (int i = 0; i < PAGES; i += 2) {
+            bf16x4_t x[CT], y[CT];
+#pragma unroll
+            for (int t = 0; t < CT; ++t) x[t] = pop[t][i], y[t] = pop[t][i + 1];
+            add_two(i, x, y);
+          }
+        }
       }
     }
   }
 
-  // The drafts of the share, 16 at a time.
+  // The drafts of the share, 16 at a time (before the pages, with those on
+  // their way, is 1 us less for one sequence and 2 us more for eight: registers).
   for (int b = max(b0, np); b < b1; ++b) {
     const int u0 = (b - np) * kPage, nv = min(k.drafts - u0, kPage);
     const size_t stride = (size_t)Hkv * D;
@@ -440,7 +488,7 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
     bf16x4_t pop[CT][1];
     const float none[1] = {1.f};
 #pragma unroll
-    for (int t = 0; t < CT; ++t) softmax_step<D, CT, 1, false, FP8>(st, t, s[t], none, pop[t]);
+    for (int t = 0; t < CT; ++t) softmax_step<D, CT, 1, false, FP8>(st, t, s[t], none, pop[t], [] {});
     wave_lds_sync();
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
@@ -480,7 +528,10 @@ __device__ __forceinline__ void split_unit(const TreeArgs& a, const Keys& k, int
     uint16_t* ql = reinterpret_cast<uint16_t*>(sm.buf) + kWaves * G::STAGE;
     for (int i = tid; i < G::COLS * (D / 8); i += 64 * kWaves) {
       const int c = i / (D / 8), d = i % (D / 8) * 8, row = sm.row[c];
-      *reinterpret_cast<u32x4_t*>(ql + c * G::QPITCH + d) = piece(a.q + (size_t)max(row, 0) * D + d, row >= 0);
+      // In the order of the reads, 8 elements of the four quads side by side.
+      const int quad_ = d / G::EPL % 4, jh = d / G::EPL / 4 * (G::EPL / 8) + d % G::EPL / 8;
+      *reinterpret_cast<u32x4_t*>(ql + c * G::QPITCH + jh * 32 + quad_ * 8) =
+          piece(a.q + (size_t)max(row, 0) * D + d, row >= 0);
     }
     __syncthreads();
   }
@@ -640,7 +691,7 @@ __device__ __forceinline__ void add_rows(const uint16_t* kst, const float (&km)[
       }
   }
 #pragma unroll
-  for (int t = 0; t < RT; ++t) softmax_step<D, RT, 2, SCALED, FP8>(st, t, s[t], vs, pop[t]);
+  for (int t = 0; t < RT; ++t) softmax_step<D, RT, 2, SCALED, FP8>(st, t, s[t], vs, pop[t], [] {});
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
     const bf16x8_t vo = RT == 1 ? vpre[dt] : read_vop(dt);
@@ -773,9 +824,7 @@ __device__ __forceinline__ void rows_unit(const TreeArgs& a, const Keys& k, int 
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) {
           u32x4_t* dst = reinterpret_cast<u32x4_t*>(kst + (only_v || i == 1 ? L::kElems : 0) + L::row(r) + col);
-          const u32x4_t w = ok ? x[i] : u32x4_t{0, 0, 0, 0};
-          dst[0] = decode8(w.x, w.y);
-          dst[1] = decode8(w.z, w.w);
+          store_decoded(dst, ok ? x[i] : u32x4_t{0, 0, 0, 0}, tid & 1);
         }
         load(blk + DEPTH, x);
         block_sync();  // the block is there, and the one before has been read
@@ -1039,13 +1088,15 @@ __device__ inline bool seq_unit(const TreeArgs& a, int u, int c0, bool note, Ord
   if (piece_id < 0) return false;
   x.h = u % Hkv;
   int s = u % per_piece / Hkv;
-  if (a.ordered && piece_id == 0) s = ranked_sequence(a, s, order);
+  if (a.longest_first > 0 && piece_id == 0)
+    s = ranked_sequence(a, s < a.longest_first ? s : a.num_seqs - 1 - (s - a.longest_first), order);
   const int2 dr = drafts_of(a, s);
+  const int g = clamp_group(a.seq_to_group[s], a.num_groups);
+  const SeqPages n = seq_pages(a, s, g);  // requested with the others, before any of them is used
+  __builtin_amdgcn_sched_barrier(0);
   x.token0 = dr.x;
   x.tokens = dr.y;
   if (c0 >= dr.y << a.rep_shift) return false;
-  const int g = clamp_group(a.seq_to_group[s], a.num_groups);
-  const SeqPages n = seq_pages(a, s, g);
   const int before = a.share ? 0 : n.prefix, total = before + n.resp;
   const int pieces = max(cdiv(total, a.piece_pages), 1);
   if (piece_id >= pieces) return false;
