@@ -623,9 +623,11 @@ struct RowsSmem {
   static constexpr int STAGES = FP8 ? 2 : 3;
   static constexpr int COLS = 64 * RT;
   __attribute__((aligned(16))) uint16_t stage[STAGES * KeyStage<D>::kStage];
-  unsigned long long mask[COLS];
+  union {
+    unsigned long long mask[COLS];
+    int token[COLS];  // of a prefix's columns, which have no drafts to see
+  };
   int row[COLS];
-  int token[COLS];
   int sum[kWaves];
   int odd[kWaves];
   int page[kTreeUnitPages];                    // page ids of the unit
@@ -893,8 +895,8 @@ __device__ __forceinline__ void rows_unit(const TreeArgs& a, const Keys& k, int 
         odd &= odd - 1;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-          const uint2 w = __builtin_bit_cast(uint2, u & 16 ? pop[t][1] : pop[t][0]);
-          const uint32_t word = u & 2 ? w.y : w.x;
+          const uint2 w0 = __builtin_bit_cast(uint2, pop[t][0]), w1 = __builtin_bit_cast(uint2, pop[t][1]);
+          const uint32_t word = u & 16 ? (u & 2 ? w1.y : w1.x) : (u & 2 ? w0.y : w0.x);
           const float p = __shfl(u & 1 ? bf16_hi(word) : bf16_lo(word), (u >> 2 & 3) * 16 + r16);
           const bool ok = seen[t] >> u & 1;
 #pragma unroll
