@@ -343,8 +343,8 @@ rp_status qk_prep_args(const rp_paged_kv* kv, const rp_group_layout* l, const Sh
   return RP_OK;
 }
 
-// Units of a tree attention: two workgroups per compute unit of an MI355X,
-// which read as fast as more of them and leave the shorter end. us a call with
+// How a tree attention is divided. Its forms' lines are at the kernels.
+// kTreeUnits units are two workgroups per compute unit of an MI355X, which read as fast as more of them and leave the shorter end. us a call with
 // 256, 512, 1024 and 2048 units at most (Hq 16, Hkv 8, d 128; sequences x
 // drafts over tokens):
 //   16 x 1-16 over 512 + U[0, 6016]:  55.3  47.9  52.5  55.7
@@ -355,20 +355,20 @@ rp_status qk_prep_args(const rp_paged_kv* kv, const rp_group_layout* l, const Sh
 //   1 x 8 over 16000:                 25.1  25.9  26.0  25.5
 // A unit below 32 pages costs more in partial results than it gives (the last
 // one with 16-page units 31.8).
-constexpr long long kTreeUnits = 512;
-constexpr int kTreeLeastPages = 32;
-
-// How a tree attention is divided, from host scalars alone. Its forms' lines
-// are at the kernels. Prefixes are either units of their own, read once for all
-// members, or part of every member's pages, read again from the caches: at
-// about 14 TB/s, against the partial results that units of their own write and
-// read, at about 1.2 TB/s, and the second launch where nothing else needs it.
+// What depends on the lengths is decided on the device: the host has the
+// tables' widths, which are often many times the lengths, and bounds from them.
+// Prefixes are either units of their own, read once for all members, or part of
+// every member's pages, read again from the caches: at about 14 TB/s, against
+// the partial results that units of their own write and read, at about 1.2
+// TB/s, and the second launch where nothing else needs it.
+constexpr int kTreeLongPages = 480;
 struct TreePlan {
   rp::TreeForm form;
   bool share;
-  int longest_first, row_blocks, chunk, max_pc, piece, max_pieces, ppr, repeats;
-  long long prefix_blocks, blocks;
-  size_t parts, part_o, part_lse, total;
+  int longest_first, row_blocks, max_pc, repeats, seq_pieces, max_extra, slots, slot_rows, least_pages;
+  float piece_share;
+  long long prefix_blocks, blocks, pieces_at;
+  size_t parts, part_o, part_lse, total;  // total 0: every result is final
 };
 
 rp_status check_tree(const Shape& sh, const rp_draft_tree* t) {
@@ -395,49 +395,66 @@ bool tree_plan(const Shape& sh, const rp_draft_tree* t, TreePlan* p) {
                          : TreeForm::kRows;
   const int cols = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128, prefix_cols = rows <= 64 ? 64 : 128;
   p->row_blocks = rp::cdiv(rows, cols);
-  // Pages of a unit where `count` units of `pages` pages would be the whole
-  // launch: few and long, as many as the chip takes at once.
-  const auto unit_pages = [](int pages, long long count) {
-    const int pieces = (int)std::max(1ll, kTreeUnits / std::max(count, 1ll));
-    return std::min(std::max(rp::cdiv(rp::cdiv(pages, pieces), 16) * 16, kTreeLeastPages), rp::kTreeUnitPages);
-  };
+  // Pieces of each of `count` where they are the whole launch.
+  const auto pieces_of = [](long long count) { return (int)(rp::kTreeUnits / std::min(std::max(count, 1ll), (long long)rp::kTreeUnits)); };
   const long long base = pairs * p->row_blocks;
   const long long per_group = (T * sh.nrep + (long long)sh.G * prefix_cols - 1) / ((long long)sh.G * prefix_cols);
   p->repeats = (int)std::min(std::max(per_group, 1ll), 64ll);
-  p->chunk = unit_pages(std::max(sh.max_pp, 1), (long long)sh.G * sh.Hkv * p->repeats);
-  p->max_pc = rp::cdiv(sh.max_pp, p->chunk);
+  p->max_pc = std::min(rp::cdiv(sh.max_pp, rp::kTreeLeastPages), pieces_of((long long)sh.G * sh.Hkv * p->repeats));
+  p->seq_pieces = pieces_of(base);
+  // Up to half a round of units for the sequences' short pieces, and the whole
+  // launch is one round; behind that, four fifths of a round and no pieces
+  // below 480 pages (7680 tokens), which cost more in partial results. us with
+  // shares of 1, 1.25 and 2 places' pages (Hq 16, Hkv 8, d 128):
+  //   16 x 1-16 over 512 + U[0, 6016]:  58 47 47 (1.14)
+  //   32 x 8 over 512 + U[0, 6016]:     95 87 88 (1.33)
+  //   32 x 8 over U[0, 30000]:          394 430 353 (1.33)
+  //   64 x 1-32, fp8, over 256 + U[8192, 32768]:  563 549 590
+  //   64 x 16, fp8, over U[0, 32768]:   430 390 426
+  const double places = base <= rp::kTreeUnits / 2 ? rp::kTreeUnits - base / 2.0 : rp::kTreeUnits / 1.25;
+  p->piece_share = (float)((double)sh.Hkv * p->row_blocks / places);
+  p->least_pages = p->seq_pieces > 1 ? rp::kTreeLeastPages : kTreeLongPages;
+  // The bound of find_piece's pieces besides the first ones.
+  const auto extra = [&](int pages) -> int {
+    if (sh.S > rp::kTreeOrderSeqs) return 0;
+    const long long by_width = (long long)sh.S * (rp::cdiv(std::max(pages, 1), p->least_pages) - 1);
+    const long long by_number = std::max((long long)sh.S * (p->seq_pieces - 1), rp::kTreeUnits / ((long long)sh.Hkv * p->row_blocks));
+    return (int)std::min(by_width, by_number);
+  };
   // Shared prefixes or not, in us.
-  const int flat_pages = std::max(sh.max_pp + sh.max_rp, 1);
+  const int flat_pages = sh.max_pp + sh.max_rp;
   const double page_bytes = 2.0 * rp::kPage * sh.D * (sh.fp8 ? 1 : 2);
   const double again = (sh.S - std::min(sh.G, sh.S)) * (double)sh.max_pp * sh.Hkv * page_bytes / 14e6;
-  const double parts = (double)T * sh.Hq * p->max_pc * sh.D * 8 / 1.2e6 +
-                       (flat_pages <= unit_pages(flat_pages, base) ? 6.0 : 0.0);
+  const double parts = (double)T * sh.Hq * (p->max_pc + (p->seq_pieces == 1 ? 1 : 0)) * sh.D * 8 / 1.8e6 +
+                       (extra(flat_pages) == 0 ? 6.0 : 0.0);
   p->share = again > parts;
   if (!p->share) p->max_pc = 0;
-  const int pages = p->share ? std::max(sh.max_rp, 1) : flat_pages;
-  p->piece = unit_pages(pages, base);
-  p->max_pieces = rp::cdiv(pages, p->piece);
-  p->ppr = p->max_pc + p->max_pieces;
-  if (p->ppr == 1) p->ppr = 0;  // every result is final
+  const int pages = p->share ? sh.max_rp : flat_pages;
+  p->max_extra = extra(pages);
   // The longest first; where one unit per sequence and kv-head fills the chip
   // once, two to a compute unit, the second one there has the shorter the
   // longer the first is (64 sequences of U[0, 7600] tokens, 8 kv-heads: as they
   // come 200 us, so 165; 32 of 1024 + U[0, 2048] with 64 drafts 135 and 119).
   p->longest_first = 0;
-  if (sh.S <= rp::kTreeOrderSeqs && base > kTreeUnits) p->longest_first = sh.S;
-  if (sh.S <= rp::kTreeOrderSeqs && base <= kTreeUnits && base > kTreeUnits / 2 && p->max_pieces == 1 && pages >= 64)
-    p->longest_first = (int)((sh.S * (kTreeUnits / 2) + base - 1) / base);
+  if (sh.S <= rp::kTreeOrderSeqs && base > rp::kTreeUnits) p->longest_first = sh.S;
+  if (sh.S <= rp::kTreeOrderSeqs && base <= rp::kTreeUnits && base > rp::kTreeUnits / 2 && pages >= 64)
+    p->longest_first = (int)((sh.S * (rp::kTreeUnits / 2) + base - 1) / base);
+  // Slots of partial results: the pieces besides the first ones, and as many
+  // first ones, or where prefixes are shared those of all sequences.
+  p->slots = p->max_extra + (p->share ? sh.S : p->max_extra);
+  p->slot_rows = rows;
+  p->pieces_at = T * sh.Hq * p->max_pc;
   const auto grid = [](long long units, long long repeats) { return (units + 7) / 8 * 8 * repeats; };
   p->prefix_blocks = p->share ? grid((long long)sh.G * p->max_pc * sh.Hkv, p->repeats) : 0;
-  p->blocks = p->prefix_blocks + grid(pairs * p->max_pieces, p->row_blocks);
-  const long long slots = T * sh.Hq * p->ppr;
-  if (T * sh.Hq >= (1ll << 31) || slots >= (1ll << 31) || T * sh.Hq * (sh.D / 4) / 256 >= rp::kMaxBlocks256 ||
+  p->blocks = p->prefix_blocks + grid(((long long)sh.S + p->max_extra) * sh.Hkv, p->row_blocks);
+  const long long partial = p->pieces_at + (long long)p->slots * sh.Hkv * rows;
+  if (T * sh.Hq >= (1ll << 31) || partial >= (1ll << 31) || T * sh.Hq * (sh.D / 4) / 256 >= rp::kMaxBlocks256 ||
       p->blocks > rp::kMaxBlocks256)
     return false;
   size_t o = 0;
-  p->parts = o;    o = align_up(o + (p->ppr == 0 ? 0 : sizeof(int) * (size_t)T));
-  p->part_o = o;   o = align_up(o + sizeof(float) * (size_t)slots * sh.D);
-  p->part_lse = o; o = align_up(o + sizeof(float) * (size_t)slots);
+  p->parts = o;    o = align_up(o + (partial == 0 ? 0 : sizeof(int4) * (size_t)T));
+  p->part_o = o;   o = align_up(o + sizeof(float) * (size_t)partial * sh.D);
+  p->part_lse = o; o = align_up(o + sizeof(float) * (size_t)partial);
   p->total = o;
   return true;
 }
@@ -663,23 +680,27 @@ rp_status rp_group_tree_attn(const rp_paged_kv* kv, const rp_group_layout* l, co
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
   char* b = static_cast<char*>(ws);
-  if (p.ppr > 0) {
-    a.token_parts = reinterpret_cast<int*>(b + p.parts);
+  if (p.total > 0) {
+    a.token_parts = reinterpret_cast<int4*>(b + p.parts);
     a.part_o = reinterpret_cast<float*>(b + p.part_o);
     a.part_lse = reinterpret_cast<float*>(b + p.part_lse);
   }
   a.share = p.share ? 1 : 0;
   a.longest_first = p.longest_first;
-  a.prefix_chunk = p.chunk;
   a.max_prefix_chunks = p.max_pc;
   a.prefix_repeats = p.repeats;
   a.prefix_blocks = (int)p.prefix_blocks;
-  a.piece_pages = p.piece;
-  a.max_pieces = p.max_pieces;
+  a.seq_pieces = p.seq_pieces;
+  a.least_pages = p.least_pages;
+  a.piece_share = p.piece_share;
+  a.max_extra = p.max_extra;
+  a.pieces_at = p.pieces_at;
+  a.slots = p.slots;
+  a.slot_rows = p.slot_rows;
   a.row_blocks = p.row_blocks;
   hipError_t e = rp::launch_tree_attn(a, sh.D, sh.fp8, p.form, p.blocks, stream);
   if (e != hipSuccess) return hip_fail(e, "tree attention kernel launch");
-  if (p.ppr == 0) return RP_OK;
+  if (p.total == 0) return RP_OK;
   e = rp::launch_tree_merge(a, sh.D, stream);
   return e == hipSuccess ? RP_OK : hip_fail(e, "tree merge kernel launch");
 }

@@ -144,13 +144,12 @@ struct PrefillArgs {
 constexpr long long kMaxBlocks256 = (1ll << 24) - 1;
 
 // Waves of a workgroup of the tree attention, and the forms of its units (keys
-// split between waves of 1 or 2 column tiles; 1 or 2 row tiles per wave over
-// shared keys). Most pages of a unit: in the split form a wave holds the page
-// ids of its share, 128 at most, a quarter of the pages and of the (at most
-// four) blocks of drafts; in the other they are in LDS.
+// split between waves of 1, 2 or 4 column tiles; row tiles over shared keys).
 constexpr int kTreeWaves = 4;
 enum class TreeForm { kSplit1, kSplit2, kSplit4, kRows };
-constexpr int kTreeUnitPages = 480;
+// Units that fill the chip, two workgroups to a compute unit, and the fewest
+// pages of a piece.
+constexpr int kTreeUnits = 512, kTreeLeastPages = 32;
 constexpr int kTreeMaxDrafts = 64;
 // Most sequences that a launch orders by length.
 constexpr int kTreeOrderSeqs = 1024;
@@ -180,18 +179,23 @@ struct TreeArgs {
   float qk_scale;                    // softmax_scale * log2(e)
   uint16_t* out;                     // bf16 [T][Hq][D]
   float* lse;                        // [T][Hq] or null
-  // Partial results (null where every row has one unit): slot k of a row, its
-  // prefix chunks first, then its sequence's pieces, at k * T * Hq + the row's place among
-  // (kv-head, draft, query head of the kv-head), so that a unit's rows follow
-  // each other.
-  float* part_o;                     // [slots][T * Hq][D]
-  float* part_lse;                   // [slots][T * Hq]
-  int* token_parts;                  // [T] partial results of each row of a token, 0: it is stored already
+  // Partial results (null where every row has one unit), rows in the order of
+  // (kv-head, token, query head of the kv-head): of max_prefix_chunks chunks of
+  // prefixes, T * Hq rows each, then from row pieces_at on of the sequences'
+  // pieces, slots * Hkv times slot_rows = max_drafts * (Hq / Hkv) rows.
+  float* part_o;                     // [rows][D]
+  float* part_lse;                   // [rows]
+  // [T]: pieces of the token's sequence (0: its rows are stored already), chunks
+  // of its prefix << 16 | place among the drafts, slot of the first piece, of the second
+  int4* token_parts;
+  long long pieces_at;
+  int slots, slot_rows;
   // How the launch is divided.
   int share;                         // prefixes are units of their own, for all members at once
   int longest_first;                 // so many sequences by decreasing length, the others by increasing; 0: as they are
-  int prefix_chunk, max_prefix_chunks, prefix_repeats, prefix_blocks;
-  int piece_pages, max_pieces, row_blocks;
+  int max_prefix_chunks, prefix_repeats, prefix_blocks;
+  int seq_pieces, least_pages, max_extra, row_blocks;
+  float piece_share;                 // pages of a piece over those of all sequences
 };
 
 // K/V rows into the cache by slot.
@@ -249,7 +253,7 @@ hipError_t launch_attn_parts(const AttnArgs& a, int head_dim, int n_rep, bool fp
 hipError_t launch_attn_small(const AttnArgs& a, const PlanArgs& p, int head_dim, int n_rep, bool fp8, void* out,
                              float* lse, hipStream_t stream);
 hipError_t launch_combine(const CombineArgs& a, int head_dim, hipStream_t stream);
-// The second launch, unless the form is whole: merges the partial results.
+// The second launch, where rows may have several units: merges the partial results.
 hipError_t launch_tree_merge(const TreeArgs& a, int head_dim, hipStream_t stream);
 hipError_t launch_tree_attn(const TreeArgs& a, int head_dim, bool fp8, TreeForm form, long long blocks,
                             hipStream_t stream);

@@ -103,6 +103,38 @@ def test_many_sequences_of_all_lengths():
     check_tree(wl, np.ones(1100, int), 6, "tree 1100 sequences", max_drafts=1)
 
 
+FORMS = [(1, 1, 16), (2, 1, 16), (4, 1, 16), (8, 1, 16)]  # of 16, 32, 64 and 128 query rows
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,n", FORMS)
+def test_sequences_of_a_thousand_pages_undivided(hq, hkv, n, d, dtype):
+    """More sequences than are ordered or divided: long ones are one unit each."""
+    rng = np.random.default_rng(n + hq)
+    L, counts = rng.integers(0, 30, 1030), np.where(np.arange(1030) % 9 == 0, 1, 0)
+    L[[3, 500, 1029]], counts[[3, 500, 1029]] = [8190, 16399, 9000], [n, n - 1, 2]
+    wl = _wl(hq, hkv, d, dtype, [0] * 1029 + [1], [20, 4], L, seed=5)
+    check_tree(wl, counts, 6, f"tree undivided {hq} {hkv} {n} {d} {dtype}", max_drafts=n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("hq,hkv,n", FORMS)
+@pytest.mark.parametrize("S,prefix", [(300, 20), (70, 20), (70, 1500), (600, 40)])
+def test_long_sequences_among_short_ones(S, prefix, hq, hkv, n, dtype):
+    """A few long sequences, first, last and with an empty tree, are divided; the others are one unit each. Tables
+    as wide as the longest and wider, prefixes read once for all or with each sequence."""
+    rng = np.random.default_rng(S + n)
+    L, counts = rng.integers(0, 60, S), rng.integers(0, 3, S)
+    at = [0, 31, S // 2, S - 1]
+    L[at], counts[at] = [9001, 30000, 7680 - prefix, 20000], [2, n, 3, 0 if S == 70 else 1]
+    groups = np.where(np.arange(S) % 5 == 2, 1, 0)
+    heads = 4 if S == 70 else 1
+    for width in (None, 4000):
+        wl = _wl(heads * hq, heads * hkv, 64, dtype, groups, [prefix, 0], L, seed=5, max_resp_pages=width)
+        check_tree(wl, counts, 6, f"tree uneven {S} {prefix} {hq} {n} {dtype} width {width}", max_drafts=n)
+
+
 @pytest.mark.parametrize("width", [None, WIDE])
 @pytest.mark.parametrize("dtype", ["bf16", "fp8"])
 def test_masks_of_any_kind(dtype, width):
