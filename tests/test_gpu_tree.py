@@ -206,6 +206,30 @@ def test_large_scores_and_a_dominant_key():
     compare_tree(out, lse, ref, 128, "large scores")
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,n", FORMS)
+def test_scales_of_fp8_pages(hq, hkv, n, d):
+    """Scales of very different sizes and of zero; a lone key's value comes out with no rounding but the output's."""
+    wl = _wl(hq, hkv, d, "fp8", np.arange(6), [0] * 6, [1, 1, 1, 300, 40, 16], seed=n + d)
+    rng = np.random.default_rng(3)
+    wl.v_scale *= np.exp2(rng.uniform(-40, 3, wl.v_scale.shape)).astype(np.float32)
+    wl.v_scale[wl.resp_block_table[3][2:5]] = 0
+    wl.v_scale[wl.resp_block_table[5][0]] = 0
+    wl.k_scale[wl.resp_block_table[3][4:7]] = 0
+    counts = [n, 1, 2, n, 3, 1]
+    dr = drafts_for(wl, counts, 4)
+    lone = dr["draft_offs"][3]
+    dr["masks"][:lone] = 0
+    dr["masks"][-1] = 0  # sees a page of zeros alone
+    say(f"tree scales hq {hq} n {n} d {d}")
+    _, out, lse = run_tree(wl, dr, n)
+    ref = oracle.tree_for_workload(wl, **dr)
+    compare_tree(out, lse, ref, d, "scales")
+    # fp32 steps of the division by the scale and by the sum: less than 2^-10 of the rounding.
+    assert np.all(np.abs(out[:lone] - ref[0][:lone]) <= 2.0 ** -8 * (1 + 2.0 ** -10) * np.abs(ref[0][:lone]))
+    assert np.all(out[-1] == 0)
+
+
 @pytest.mark.parametrize("width", [None, WIDE])
 def test_rows_behind_the_last_sequence_stay(width):
     import paper_2606_26997_amd as rp
