@@ -314,15 +314,15 @@ def validate_layout(kv, layout, stream=None) -> None:
 
 
 def _tensors(*specs) -> None:
-    """Refuse tensors that the library would read as others: (name, tensor, dtype, shape), with None for a size
-    that may be any. Raw addresses (int) and None pass; every tensor is on the current device."""
+    """Refuse tensors that the library would read as others: (name, tensor, dtype, shape), with None for what may
+    be any. Raw addresses (int) and None pass; every tensor is on the current device."""
     device = None
     for name, t, dtype, shape in specs:
         if t is None or isinstance(t, int):
             continue
-        if t.dtype is not dtype:
+        if dtype is not None and t.dtype is not dtype:
             raise ValueError(f"{name}: dtype {t.dtype}, not {dtype}")
-        if t.shape != shape and (t.dim() != len(shape) or any(w not in (None, g) for g, w in zip(t.shape, shape))):
+        if shape is not None and t.shape != shape and (t.dim() != len(shape) or any(w not in (None, g) for g, w in zip(t.shape, shape))):
             raise ValueError(f"{name}: shape {tuple(t.shape)}, not {shape}")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous (strides {t.stride()})")
@@ -337,8 +337,10 @@ def draft_tree(draft_offs, masks, *, max_drafts, num_drafts=None) -> RpDraftTree
     masks (int64 or uint64 [T]) say which drafts of its sequence each one sees, bit u for the u-th."""
     _tensors(("draft_offs", draft_offs, torch.int32, (None,)),
              ("masks", masks, torch.uint64 if getattr(masks, "dtype", None) is torch.uint64 else torch.int64, (None,)))
-    return RpDraftTree(int(masks.shape[0]) if num_drafts is None else int(num_drafts), int(max_drafts),
-                       _ptr(draft_offs), _ptr(masks))
+    T = int(masks.shape[0]) if num_drafts is None else int(num_drafts)
+    if not isinstance(masks, int) and T > masks.shape[0]:
+        raise ValueError(f"num_drafts {T}, but masks has {masks.shape[0]} entries")
+    return RpDraftTree(T, int(max_drafts), _ptr(draft_offs), _ptr(masks))
 
 
 def group_tree_attn_workspace_size(kv, layout, tree) -> int:
@@ -354,7 +356,7 @@ def group_tree_attn(kv, layout, tree, q, k_draft, v_draft, softmax_scale, out, l
     T, hq, hkv, d = tree.num_drafts, layout.num_q_heads, kv.num_kv_heads, kv.head_dim
     bf16 = torch.bfloat16
     _tensors(("q", q, bf16, (T, hq, d)), ("k_draft", k_draft, bf16, (T, hkv, d)), ("v_draft", v_draft, bf16, (T, hkv, d)),
-             ("out", out, bf16, (T, hq, d)), ("lse", lse, torch.float32, (T, hq)))
+             ("out", out, bf16, (T, hq, d)), ("lse", lse, torch.float32, (T, hq)), ("workspace", workspace, None, None))
     _check(load().rp_group_tree_attn(ctypes.byref(kv), ctypes.byref(layout), ctypes.byref(tree), _ptr(q),
                                      _ptr(k_draft), _ptr(v_draft), float(softmax_scale), _ptr(out), _ptr(lse),
                                      _ptr(workspace), _ws_bytes(workspace), _stream(stream)), "rp_group_tree_attn")

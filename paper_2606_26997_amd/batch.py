@@ -199,7 +199,7 @@ class PageTables:
         device whether it was done; the lengths follow only then, and ``slot_map`` has the new tokens' slots."""
         B.page_tables_resize(self.tables, self.lens, new_lens, self.status, self.slot_offs, slot_map, stream)
         if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream)
+            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
         with torch.cuda.stream(stream):  # None: the current one
             self.lens.copy_(torch.where(self.status[0] == B.RP_TABLES_OK, new_lens, self.lens))
 

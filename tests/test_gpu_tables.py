@@ -170,3 +170,17 @@ def test_the_handle_keeps_its_lengths_when_a_call_is_refused():
     assert pt.status.tolist() == [0, 3, 0, 20] and more.status.tolist() == [1, 1, 0, 1]
     assert pt.lens.tolist() == [17, 3] and more.lens.tolist() == [0]
     assert pt.block_table[:, :2].tolist() == [[0, 1], [2, -1]]
+
+
+def test_the_handle_on_streams_given_by_address():
+    import paper_2606_26997_amd as rp
+    pt = rp.PageTables(num_seqs=2, max_pages=4, num_pages=8)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    lens = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([20, 3], [33, 40], [0, 16])]
+    torch.cuda.synchronize()
+    for x, stream in zip(lens, (0, side.cuda_stream, side)):
+        pt.resize(x, stream=stream)
+        torch.cuda.synchronize()
+        assert pt.status.tolist()[0] == rp.RP_TABLES_OK and torch.equal(pt.lens, x)
+    assert pt.stack[1].item() == 7

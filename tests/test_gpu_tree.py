@@ -322,3 +322,36 @@ def test_repeats_and_graph_replays_are_equal(dtype, width):
         b.tree_attention()
         torch.cuda.synchronize()
         first = b.draft_out.clone(), b.draft_lse.clone()
+
+
+def test_two_calls_at_once():
+    """Two streams, each with its own workspace, on one cache: both results are those of the calls one after the
+    other."""
+    import paper_2606_26997_amd as rp
+    say("tree two streams")
+    wl = _wl(8, 4, 64, "bf16", [0, 1, 0, 1], [300, 17], [5000, 2000, 0, 9000], seed=8)
+    cases = [(drafts_for(wl, counts, i), max(counts)) for i, counts in enumerate(([4, 1, 9, 16], [30, 2, 1, 0]))]
+    want = [run_tree(wl, dr, most)[1:] for dr, most in cases]
+    batches = []
+    for dr, most in cases:
+        b = rp.DeviceBatch.from_workload(wl)
+        b.set_drafts(**{**dr, "masks": dr["masks"].view(np.int64)}, max_drafts=most)
+        batches.append((b, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for b, stream in batches:
+            with torch.cuda.stream(stream):
+                b.draft_out.zero_()
+                b.tree_attention()
+        torch.cuda.synchronize()
+        for (b, _), (out, lse) in zip(batches, want):
+            assert np.array_equal(b.draft_out.float().cpu().numpy().astype(np.float64), out)
+            assert np.array_equal(b.draft_lse.cpu().numpy().astype(np.float64), lse)
+
+
+def test_the_binding_refuses_more_drafts_than_masks():
+    import paper_2606_26997_amd as rp
+    offs, masks = (torch.zeros(3, dtype=t, device="cuda") for t in (torch.int32, torch.int64))
+    with pytest.raises(ValueError, match="masks has 3"):
+        rp.draft_tree(offs, masks, max_drafts=2, num_drafts=4)
+    assert rp.draft_tree(offs, masks, max_drafts=2, num_drafts=2).num_drafts == 2

@@ -136,7 +136,8 @@ def test_the_binding_refuses_tensors_of_another_kind():
     args = dict(q=A, k_draft=A, v_draft=A, softmax_scale=0.1, out=A, lse=None, workspace=None)
     for name, t, needle in (("q", q.float(), "dtype"), ("q", q[:4], "shape"), ("k_draft", q, "shape"),
                             ("q", torch.zeros(8, 64, 4, dtype=torch.bfloat16).transpose(1, 2), "contiguous"),
-                            ("q", q, "current GPU")):
+                            ("q", q, "current GPU"), ("workspace", torch.zeros(8, 2)[:, 0], "contiguous"),
+                            ("workspace", q, "current GPU")):
         with pytest.raises(ValueError, match=needle):
             rp.group_tree_attn(kv, layout, tree, **{**args, name: t})
     with pytest.raises(ValueError, match="dtype"):
