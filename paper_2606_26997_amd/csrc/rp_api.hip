@@ -343,29 +343,50 @@ rp_status qk_prep_args(const rp_paged_kv* kv, const rp_group_layout* l, const Sh
   return RP_OK;
 }
 
-// How a tree attention is divided. Its forms' lines are at the kernels.
-// kTreeUnits units are two workgroups per compute unit of an MI355X, which read as fast as more of them and leave the shorter end. us a call with
-// 256, 512, 1024 and 2048 units at most (Hq 16, Hkv 8, d 128; sequences x
-// drafts over tokens):
-//   16 x 1-16 over 512 + U[0, 6016]:  55.3  47.9  52.5  55.7
-//   16 x 32 over 512 + U[0, 6016]:    69.0  63.0  73.6  86.2
-//   8 x 8 over 512 + U[0, 16000]:     65.7  62.3  66.0  71.5
-//   16 x 8, fp8, the first's tokens:  42.5  34.9  39.8  43.5
-//   64 x 8 over U[0, 7600]:           197   199   206   199
-//   1 x 8 over 16000:                 25.1  25.9  26.0  25.5
-// A unit below 32 pages costs more in partial results than it gives (the last
-// one with 16-page units 31.8).
-// What depends on the lengths is decided on the device: the host has the
-// tables' widths, which are often many times the lengths, and bounds from them.
+// How a tree attention is divided. What depends on the lengths is decided on
+// the device: the host has the tables' widths, which are often many times the
+// lengths, and bounds from them.
+//
+// kTreeUnits units are two workgroups per compute unit of an MI355X, which read
+// as fast as more of them and leave the shorter end. us a call with 256, 512,
+// 1024 and 2048 of them (Hq 16, Hkv 8, d 128; sequences x drafts over tokens):
+//   16 x 1-16 over 512 + U[0, 6016]:  45.3  45.1  53.0  53.1
+//   16 x 32 over 512 + U[0, 6016]:    63.3  57.6  79.7  79.7
+//   8 x 8 over 512 + U[0, 16000]:     52.9  54.9  56.9  64.1
+//   16 x 8, fp8, the first's tokens:  38.3  31.1  39.3  39.5
+//   64 x 8 over U[0, 7600]:           205   174   210   203
+// A piece of fewer than 32 pages costs more in partial results than it gives,
+// of more too few units for small calls (4 x 8 over 512 + U[0, 6016], 16, 32
+// and 64 pages: 24.3 21.2 26.3).
+//
+// Forms, by the query rows of a (sequence, kv-head): one, two or four tiles of
+// 16 with the keys split between waves up to 64 rows, keys shared by waves
+// beyond. us with 1, 2, 4 tiles and shared keys (64 sequences, 8 kv-heads, d
+// 64, 8192 tokens; bf16, then fp8):
+//   16 rows   180 183 184 201   105 107 109 181
+//   32 rows   264 190 188 205   149 113 115 183
+//   64 rows   446 282 204 228   254 177 148 219
+//   96 rows   634 388 308 254   363 253 259 234
+//   128 rows  765 475 325 270   481 326 274 252
+// and with d 128 (bf16 10240, fp8 20480 tokens) at 16 rows 440-456 against
+// 430-460 with two tiles, at 32 441-473 against 610-640 with one, at 64 480 (fp8
+// 592-615) against 506-520 (740) with shared keys, at 96 520 (815) with shared
+// keys against 680 (1060) with four tiles.
+//
 // Prefixes are either units of their own, read once for all members, or part of
 // every member's pages, read again from the caches: at about 14 TB/s, against
-// the partial results that units of their own write and read, at about 1.2
-// TB/s, and the second launch where nothing else needs it.
+// the partial results that units of their own write and read (those of the
+// prefix, and those of the pieces where these would be final), at about 1.8
+// TB/s, and the second launch where nothing else needs it. us apart and read by
+// each (8 kv-heads, d 128):
+//   64 sequences, 512 tokens, 1, 8 and 16 drafts: 101 107, 108 106, 133 111
+//   256 sequences, 512 tokens, 2 drafts, 1024 tokens, 8 drafts: 205 232, 251 297
+//   64 sequences, 2048 tokens, 4 and 16 drafts: 40 66, 76 73
 constexpr int kTreeLongPages = 480;
 struct TreePlan {
   rp::TreeForm form;
   bool share;
-  int longest_first, row_blocks, max_pc, repeats, seq_pieces, max_extra, slots, slot_rows, least_pages;
+  int longest_first, row_blocks, max_pc, repeats, seq_pieces, max_extra, slot_rows, least_pages;
   float piece_share;
   long long prefix_blocks, blocks, pieces_at;
   size_t parts, part_o, part_lse, total;  // total 0: every result is final
@@ -439,20 +460,17 @@ bool tree_plan(const Shape& sh, const rp_draft_tree* t, TreePlan* p) {
   if (sh.S <= rp::kTreeOrderSeqs && base > rp::kTreeUnits) p->longest_first = sh.S;
   if (sh.S <= rp::kTreeOrderSeqs && base <= rp::kTreeUnits && base > rp::kTreeUnits / 2 && pages >= 64)
     p->longest_first = (int)((sh.S * (rp::kTreeUnits / 2) + base - 1) / base);
-  // Slots of partial results: the pieces besides the first ones, and as many
-  // first ones, or where prefixes are shared those of all sequences.
-  p->slots = p->max_extra + (p->share ? sh.S : p->max_extra);
   p->slot_rows = rows;
-  p->pieces_at = T * sh.Hq * p->max_pc;
+  p->pieces_at = p->share || p->max_extra > 0 ? T * sh.Hq * (p->max_pc + 1) : 0;
   const auto grid = [](long long units, long long repeats) { return (units + 7) / 8 * 8 * repeats; };
   p->prefix_blocks = p->share ? grid((long long)sh.G * p->max_pc * sh.Hkv, p->repeats) : 0;
   p->blocks = p->prefix_blocks + grid(((long long)sh.S + p->max_extra) * sh.Hkv, p->row_blocks);
-  const long long partial = p->pieces_at + (long long)p->slots * sh.Hkv * rows;
+  const long long partial = p->pieces_at + (long long)p->max_extra * sh.Hkv * rows;
   if (T * sh.Hq >= (1ll << 31) || partial >= (1ll << 31) || T * sh.Hq * (sh.D / 4) / 256 >= rp::kMaxBlocks256 ||
       p->blocks > rp::kMaxBlocks256)
     return false;
   size_t o = 0;
-  p->parts = o;    o = align_up(o + (partial == 0 ? 0 : sizeof(int4) * (size_t)T));
+  p->parts = o;    o = align_up(o + (partial == 0 ? 0 : sizeof(int2) * (size_t)T));
   p->part_o = o;   o = align_up(o + sizeof(float) * (size_t)partial * sh.D);
   p->part_lse = o; o = align_up(o + sizeof(float) * (size_t)partial);
   p->total = o;
@@ -681,7 +699,7 @@ rp_status rp_group_tree_attn(const rp_paged_kv* kv, const rp_group_layout* l, co
   a.lse = lse;
   char* b = static_cast<char*>(ws);
   if (p.total > 0) {
-    a.token_parts = reinterpret_cast<int4*>(b + p.parts);
+    a.token_parts = reinterpret_cast<int2*>(b + p.parts);
     a.part_o = reinterpret_cast<float*>(b + p.part_o);
     a.part_lse = reinterpret_cast<float*>(b + p.part_lse);
   }
@@ -695,7 +713,6 @@ rp_status rp_group_tree_attn(const rp_paged_kv* kv, const rp_group_layout* l, co
   a.piece_share = p.piece_share;
   a.max_extra = p.max_extra;
   a.pieces_at = p.pieces_at;
-  a.slots = p.slots;
   a.slot_rows = p.slot_rows;
   a.row_blocks = p.row_blocks;
   hipError_t e = rp::launch_tree_attn(a, sh.D, sh.fp8, p.form, p.blocks, stream);

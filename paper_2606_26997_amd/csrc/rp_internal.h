@@ -181,15 +181,17 @@ struct TreeArgs {
   float* lse;                        // [T][Hq] or null
   // Partial results (null where every row has one unit), rows in the order of
   // (kv-head, token, query head of the kv-head): of max_prefix_chunks chunks of
-  // prefixes, T * Hq rows each, then from row pieces_at on of the sequences'
-  // pieces, slots * Hkv times slot_rows = max_drafts * (Hq / Hkv) rows.
+  // prefixes and of the sequences' first pieces T * Hq rows each, then from row
+  // pieces_at on max_drafts * (Hq / Hkv) = slot_rows rows per other piece and
+  // kv-head.
   float* part_o;                     // [rows][D]
   float* part_lse;                   // [rows]
-  // [T]: pieces of the token's sequence (0: its rows are stored already), chunks
-  // of its prefix << 16 | place among the drafts, slot of the first piece, of the second
-  int4* token_parts;
+  // [T]: pieces of the token's sequence (0: its rows are stored already) and
+  // the token's place in its tree << 16; chunks of its prefix and the first of
+  // the other pieces << 16
+  int2* token_parts;
   long long pieces_at;
-  int slots, slot_rows;
+  int slot_rows;
   // How the launch is divided.
   int share;                         // prefixes are units of their own, for all members at once
   int longest_first;                 // so many sequences by decreasing length, the others by increasing; 0: as they are

