@@ -314,8 +314,9 @@ __device__ void tell(const TableArgs& a, const Sums& m, int status, const long l
 }
 
 // Everything in one workgroup, which is latency: lengths, sums, table entries,
-// slots, 3.8 us for 16 sequences and 136 new tokens. The slots from what the tables hold before, with
-// new pages by their rank, in the shadow of the first moves' loads.
+// slots, 3.8 us for 16 sequences and 136 new tokens. The slots come from what the
+// tables hold before, with new pages by their rank, in the shadow of the first
+// moves' loads.
 template <class Sum>
 __global__ __launch_bounds__(1024) void tables_one_kernel(const TableArgs a) {
   __shared__ Sums m;
