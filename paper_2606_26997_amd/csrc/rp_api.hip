@@ -417,7 +417,9 @@ bool tree_plan(const Shape& sh, const rp_draft_tree* t, TreePlan* p) {
   const int cols = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128, prefix_cols = rows <= 64 ? 64 : 128;
   p->row_blocks = rp::cdiv(rows, cols);
   // Pieces of each of `count` where they are the whole launch.
-  const auto pieces_of = [](long long count) { return (int)(rp::kTreeUnits / std::min(std::max(count, 1ll), (long long)rp::kTreeUnits)); };
+  const auto pieces_of = [](long long count) {
+    return (int)(rp::kTreeUnits / std::min(std::max(count, 1ll), (long long)rp::kTreeUnits));
+  };
   const long long base = pairs * p->row_blocks;
   const long long per_group = (T * sh.nrep + (long long)sh.G * prefix_cols - 1) / ((long long)sh.G * prefix_cols);
   p->repeats = (int)std::min(std::max(per_group, 1ll), 64ll);
@@ -425,7 +427,8 @@ bool tree_plan(const Shape& sh, const rp_draft_tree* t, TreePlan* p) {
   p->seq_pieces = pieces_of(base);
   // Up to half a round of units for the sequences' short pieces, and the whole
   // launch is one round; behind that, four fifths of a round and no pieces
-  // below 480 pages (7680 tokens), which cost more in partial results. us with
+  // below 480 pages (7680 tokens), which cost more in partial results (64 x 8
+  // over U[0, 7600]: 173, from 240 pages on cut 184). us with
   // shares of 1, 1.25 and 2 places' pages (Hq 16, Hkv 8, d 128):
   //   16 x 1-16 over 512 + U[0, 6016]:  58 47 47 (1.14)
   //   32 x 8 over 512 + U[0, 6016]:     95 87 88 (1.33)
@@ -439,7 +442,8 @@ bool tree_plan(const Shape& sh, const rp_draft_tree* t, TreePlan* p) {
   const auto extra = [&](int pages) -> int {
     if (sh.S > rp::kTreeOrderSeqs) return 0;
     const long long by_width = (long long)sh.S * (rp::cdiv(std::max(pages, 1), p->least_pages) - 1);
-    const long long by_number = std::max((long long)sh.S * (p->seq_pieces - 1), rp::kTreeUnits / ((long long)sh.Hkv * p->row_blocks));
+    const long long by_number = std::max((long long)sh.S * (p->seq_pieces - 1),
+                                         rp::kTreeUnits / ((long long)sh.Hkv * p->row_blocks));
     return (int)std::min(by_width, by_number);
   };
   // Shared prefixes or not, in us.

@@ -192,8 +192,8 @@ __device__ inline long long part_of(const TreeArgs& a, int row, long long base) 
 // A lane's part of row `row` (-1: none) of a 16-row tile: elements dt * 16 +
 // quad * 4 + e.
 template <int D>
-__device__ inline void store_row(const TreeArgs& a, int row, long long part, int quad, const f32x4_t (&o)[D / 16], float inv,
-                                 float lse) {
+__device__ inline void store_row(const TreeArgs& a, int row, long long part, int quad, const f32x4_t (&o)[D / 16],
+                                 float inv, float lse) {
   if (row < 0) return;
   if (part == kFinal) {
     uint16_t* dst = a.out + (size_t)row * D + quad * 4;
@@ -528,7 +528,8 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
 // A unit: the columns in sm.row over `k`, split between the waves, merged and
 // stored: final rows (slot < 0), or the partial results in their slot.
 template <int D, bool FP8, int CT>
-__device__ __forceinline__ void split_unit(const TreeArgs& a, const Keys& k, int h, long long part, Smem<D, FP8, CT>& sm) {
+__device__ __forceinline__ void split_unit(const TreeArgs& a, const Keys& k, int h, long long part,
+                                           Smem<D, FP8, CT>& sm) {
   using G = Shape<D, FP8, CT>;
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -720,7 +721,8 @@ __device__ inline void block_sync() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_ba
 
 // A unit: rows sm.row, RT tiles for each wave. Waves without rows only copy.
 template <int D, bool FP8, int RT>
-__device__ __forceinline__ void rows_unit(const TreeArgs& a, const Keys& k, int h, long long part, RowsSmem<D, FP8, RT>& sm) {
+__device__ __forceinline__ void rows_unit(const TreeArgs& a, const Keys& k, int h, long long part,
+                                          RowsSmem<D, FP8, RT>& sm) {
   using L = KeyStage<D>;
   constexpr int KB = D / 32, DT = D / 16, STAGES = RowsSmem<D, FP8, RT>::STAGES;
   constexpr int ROW_BYTES = D * (FP8 ? 1 : 2), BLOCK_BYTES = kPage * ROW_BYTES;
@@ -1260,7 +1262,8 @@ __device__ inline unsigned long long column_mask(const TreeArgs& a, const SeqUni
 // tiles take as long as the reads. Small calls are latency: lengths, then page
 // ids, then pages, 7 us for 4 sequences of 180 tokens.
 template <int D, bool FP8, int CT>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8))) void tree_split_kernel(const TreeArgs a) {
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
+void tree_split_kernel(const TreeArgs a) {
   __shared__ union U {
     Smem<D, FP8, CT> split;
     Smem<D, FP8, 2> few;
@@ -1347,12 +1350,16 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
   const int2 p = a.token_parts[t];
   if ((p.x & 0xffff) == 0) return;  // stored already
   const int sub = threadIdx.x % LPR, chunks = min(p.y & 0xffff, a.max_prefix_chunks);
-  const int extra0 = min((int)((unsigned)p.y >> 16), a.max_extra), n = chunks + 1 + min((p.x & 0xffff) - 1, a.max_extra - extra0);
+  const int extra0 = min((int)((unsigned)p.y >> 16), a.max_extra);
+  const int n = chunks + 1 + min((p.x & 0xffff) - 1, a.max_extra - extra0);
   const long long stride = (long long)a.num_kv_heads * a.slot_rows;
+  const int own = min((int)((unsigned)p.x >> 16), a.max_drafts - 1);
   const long long extra = a.pieces_at + (long long)h * a.slot_rows + (extra0 - chunks - 1) * stride +
-                          (min((int)((unsigned)p.x >> 16), a.max_drafts - 1) << a.rep_shift) + (c & ((1 << a.rep_shift) - 1));
+                          (own << a.rep_shift) + (c & ((1 << a.rep_shift) - 1));
   // Part k: a prefix chunk, the first piece, another piece.
-  const auto place = [&](int k) { return k <= chunks ? (k < chunks ? k : a.max_prefix_chunks) * rows + i : extra + k * stride; };
+  const auto place = [&](int k) {
+    return k <= chunks ? (k < chunks ? k : a.max_prefix_chunks) * rows + i : extra + k * stride;
+  };
   const f32x4_t* o = reinterpret_cast<const f32x4_t*>(a.part_o) + sub;
   float m = -INFINITY, w = 0.f;
   f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
