@@ -1256,10 +1256,10 @@ __device__ inline unsigned long long column_mask(const TreeArgs& a, const SeqUni
 }
 
 // Bound by the reads of the cache: 256 sequences of 8 drafts over 64 to 512 +
-// U[0, 4096] tokens (Hkv 8, d 128) 2.21 GB in 385 us, 5.7 TB/s, of the 7.0 that
+// U[0, 4096] tokens (Hkv 8, d 128) 2.21 GB in 380 us, 5.8 TB/s, of the 7.0 that
 // one large read reaches; 64 fp8 sequences of 1 to 32 drafts over 8192 to 32768
-// tokens 2.70 GB in 540 us, 5.0 TB/s, where decoding and the softmax of four
-// tiles take as long as the reads. Small calls are latency: lengths, then page
+// tokens 2.70 GB in 540 to 590 us, 4.6 to 5.0 TB/s, where decoding and the
+// softmax of four tiles take as long as the reads. Small calls are latency: lengths, then page
 // ids, then pages, 7 us for 4 sequences of 180 tokens.
 template <int D, bool FP8, int CT>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
