@@ -262,8 +262,9 @@ rp_status rp_group_tree_attn_workspace_size(const rp_paged_kv* kv, const rp_grou
                                             const rp_draft_tree* tree, size_t* bytes);
 
 /* Attention of every drafted token (paper, Section 4: a decode step of the
- * rollout node's workers, here over several tokens per sequence; each group's
- * prefix is still read once for all of its members, Section 2.1).
+ * rollout node's workers, here over several tokens per sequence; a group's
+ * prefix, Section 2.1, is read once for all of its members where that is
+ * faster than from the caches with each of them).
  * q: bf16 [T][Hq][head_dim]; k_draft, v_draft: bf16 [T][Hkv][head_dim], the
  * drafts' own keys and values, which are not in the cache (also for fp8
  * pools): accepted ones are written there afterwards (rp_kv_write_slots).
@@ -271,6 +272,10 @@ rp_status rp_group_tree_attn_workspace_size(const rp_paged_kv* kv, const rp_grou
  * log, may be NULL. Rows from draft_offs[S] on are neither read nor written.
  * softmax_scale must be finite and > 0. Probabilities are rounded to bf16 for
  * their product with V; sums, maxima and outputs are held in fp32.
+ * The response tables may be as wide as they like; max_prefix_pages is taken
+ * for the prefixes' length where it is decided whether they are read once for
+ * all members or with each of them (a table 64 times as wide as the prefixes
+ * costs up to a fifth).
  * workspace: device buffer of at least rp_group_tree_attn_workspace_size
  * bytes, 256-byte aligned (may be NULL when that is 0); concurrent calls need
  * distinct workspaces. */
