@@ -180,28 +180,36 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream
 
 
+def _holding(descriptor, *tensors):
+    """The descriptor, with the tensors behind its addresses alive for as long as it is."""
+    descriptor.tensors = tuple(t for t in tensors if isinstance(t, torch.Tensor))
+    return descriptor
+
+
 def paged_kv(k_pages, v_pages, k_scale=None, v_scale=None, *, num_pages=None, num_kv_heads=None,
              page_size=16, head_dim=None, kv_dtype=None) -> RpPagedKV:
     """Describe a pool of tensors shaped [num_pages][Hkv][page_size][head_dim]."""
     shape = tuple(k_pages.shape) if hasattr(k_pages, "shape") else None
     if kv_dtype is None:
         kv_dtype = RP_KV_FP8_E4M3 if k_scale is not None else RP_KV_BF16
-    return RpPagedKV(_ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale),
-                     num_pages if num_pages is not None else shape[0],
-                     num_kv_heads if num_kv_heads is not None else shape[1],
-                     page_size, head_dim if head_dim is not None else shape[3], kv_dtype)
+    kv = RpPagedKV(_ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale),
+                   num_pages if num_pages is not None else shape[0],
+                   num_kv_heads if num_kv_heads is not None else shape[1],
+                   page_size, head_dim if head_dim is not None else shape[3], kv_dtype)
+    return _holding(kv, k_pages, v_pages, k_scale, v_scale)
 
 
 def group_layout(seq_to_group, prefix_lens, prefix_block_table, resp_lens, resp_block_table, *,
                  num_q_heads, num_seqs=None, num_groups=None, max_prefix_pages=None,
                  max_resp_pages=None) -> RpGroupLayout:
-    return RpGroupLayout(
+    layout = RpGroupLayout(
         num_seqs if num_seqs is not None else seq_to_group.shape[0],
         num_groups if num_groups is not None else prefix_lens.shape[0],
         num_q_heads, _ptr(seq_to_group), _ptr(prefix_lens), _ptr(prefix_block_table),
         max_prefix_pages if max_prefix_pages is not None else prefix_block_table.shape[1],
         _ptr(resp_lens), _ptr(resp_block_table),
         max_resp_pages if max_resp_pages is not None else resp_block_table.shape[1])
+    return _holding(layout, seq_to_group, prefix_lens, prefix_block_table, resp_lens, resp_block_table)
 
 
 def kv_append(kv: RpPagedKV, layout: RpGroupLayout, k_new, v_new, stream=None) -> None:
@@ -340,7 +348,7 @@ def draft_tree(draft_offs, masks, *, max_drafts, num_drafts=None) -> RpDraftTree
     T = int(masks.shape[0]) if num_drafts is None else int(num_drafts)
     if not isinstance(masks, int) and T > masks.shape[0]:
         raise ValueError(f"num_drafts {T}, but masks has {masks.shape[0]} entries")
-    return RpDraftTree(T, int(max_drafts), _ptr(draft_offs), _ptr(masks))
+    return _holding(RpDraftTree(T, int(max_drafts), _ptr(draft_offs), _ptr(masks)), draft_offs, masks)
 
 
 def group_tree_attn_workspace_size(kv, layout, tree) -> int:
@@ -367,8 +375,9 @@ def page_tables(block_table, free_pages, free_count) -> RpPageTables:
     count, int32 [1])."""
     _tensors(("block_table", block_table, torch.int32, (None, None)), ("free_pages", free_pages, torch.int32, (None,)),
              ("free_count", free_count, torch.int32, (1,)))
-    return RpPageTables(int(block_table.shape[0]), int(block_table.shape[1]), 16, int(free_pages.shape[0]),
-                        _ptr(block_table), _ptr(free_pages), _ptr(free_count))
+    tables = RpPageTables(int(block_table.shape[0]), int(block_table.shape[1]), 16, int(free_pages.shape[0]),
+                          _ptr(block_table), _ptr(free_pages), _ptr(free_count))
+    return _holding(tables, block_table, free_pages, free_count)
 
 
 def page_tables_resize(tables, old_lens, new_lens, status, slot_offs=None, slot_map=None, stream=None) -> None:
@@ -397,8 +406,9 @@ def kv_write_slots(kv, slot_map, k_new, v_new, src_rows=None, stream=None) -> No
 
 def prefill_layout(prompt_offs, prefix_block_table, *, num_q_heads, num_tokens) -> RpPrefillLayout:
     """Describe packed prompts: group g owns rows prompt_offs[g] .. prompt_offs[g+1]-1."""
-    return RpPrefillLayout(int(prompt_offs.shape[0]) - 1, int(num_q_heads), int(num_tokens), _ptr(prompt_offs),
-                           _ptr(prefix_block_table), int(prefix_block_table.shape[1]))
+    layout = RpPrefillLayout(int(prompt_offs.shape[0]) - 1, int(num_q_heads), int(num_tokens), _ptr(prompt_offs),
+                             _ptr(prefix_block_table), int(prefix_block_table.shape[1]))
+    return _holding(layout, prompt_offs, prefix_block_table)
 
 
 def prefill_kv_write(kv, layout, k, v, stream=None) -> None:
