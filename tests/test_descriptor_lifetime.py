@@ -14,7 +14,7 @@ def _zeros(shape, dtype, device):
 
 
 def _described(device):
-    """(descriptor, weak references to every tensor that it was made from), the tensors' only other names gone."""
+    """(name, [descriptor], weak references to the tensors that it was made from, their addresses)."""
     i32, bf16, f32, u8 = torch.int32, torch.bfloat16, torch.float32, torch.uint8
     makers = {
         "paged_kv bf16": (rp.paged_kv, [((2, 1, 16, 64), bf16)] * 2, {}),
@@ -27,19 +27,17 @@ def _described(device):
     }
     for name, (make, specs, kw) in makers.items():
         tensors = [_zeros(shape, dtype, device) for shape, dtype in specs]
-        refs, addresses = [weakref.ref(t) for t in tensors], [t.data_ptr() for t in tensors]
-        desc = make(*tensors, **kw)
+        refs, addresses, box = [weakref.ref(t) for t in tensors], [t.data_ptr() for t in tensors], [make(*tensors, **kw)]
         del tensors
-        gc.collect()
-        yield name, desc, refs, addresses
+        yield name, box, refs, addresses
 
 
 def _check(device):
-    for name, desc, refs, addresses in _described(device):
+    for name, box, refs, addresses in _described(device):
+        gc.collect()
         assert all(r() is not None for r in refs), name
-        held = {getattr(desc, f) for f, _ in desc._fields_}
-        assert set(addresses) <= held, name
-        del desc
+        assert set(addresses) <= {getattr(box[0], f) for f, _ in box[0]._fields_}, name
+        box.clear()
         gc.collect()
         assert all(r() is None for r in refs), name
 
