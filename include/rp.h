@@ -337,14 +337,17 @@ rp_status rp_page_tables_resize(const rp_page_tables* tables, const int32_t* old
  * [0, num_pages * 16) or whose row is not in [0, num_src) are skipped; -1 pads.
  * A row may be written to several slots, a slot must not occur twice.
  * RP_KV_BF16: the values are copied.
- * RP_KV_FP8_E4M3: a run is a maximal stretch of entries whose slots follow each
- * other (slot + 1) inside one page; a page must have at most one run. Per run
- * and kv-head, separately for K and V, in fp32: amax = max |x| over the run's
- * rows; a run that begins in row 0 sets scale = amax / 448 (1 if amax == 0); one
- * that begins in row r > 0 keeps the scale if amax <= 448 * scale, and otherwise
- * sets scale = amax / 448 and requantises rows 0..r-1 from code * old_scale;
- * rows are stored as e4m3(x / scale), rounding and NaN as rp_kv_append's. A run
- * of one row is rp_kv_append's rule, a run from row 0 rp_prefill_kv_write's.
+ * RP_KV_FP8_E4M3: a run is a maximal stretch of entries, skipped ones left out,
+ * whose slots rise inside one page; a page must have at most one run, its first
+ * and last entry fewer than 64 places apart in the list (drafts may be given in
+ * place, -1 for those that are not accepted). Per run and kv-head, separately for
+ * K and V, in fp32: amax = max |x| over the run's rows; a run that begins in row 0
+ * sets scale = amax / 448 (1 if amax == 0); one that begins in row r > 0 keeps the
+ * scale if amax <= 448 * scale, and otherwise sets scale = amax / 448 and
+ * requantises rows 0..r-1 from code * old_scale; rows are stored as
+ * e4m3(x / scale), rounding and NaN as rp_kv_append's; the codes of other rows,
+ * those that a run passes over among them, stay. A run of one row is
+ * rp_kv_append's rule, a run from row 0 rp_prefill_kv_write's.
  * Repeating a call with the same inputs is idempotent. */
 rp_status rp_kv_write_slots(const rp_paged_kv* kv, const int32_t* slot_map, int32_t num_tokens, const void* k_new,
                             const void* v_new, const int32_t* src_rows, int32_t num_src, hipStream_t stream);

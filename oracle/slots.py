@@ -1,9 +1,10 @@
 """K/V rows written into a paged pool by slot, and block tables grown and shrunk from lengths.
 
-A slot is ``page * ps + row``. fp8 pools: a run is a maximal stretch of list entries whose slots follow each
-other inside a page; with ``amax`` over the run's rows (fp32, NaN left out), a run from row 0 sets
+A slot is ``page * ps + row``. fp8 pools: a run is a maximal stretch of list entries, skipped ones left out, whose
+slots rise inside a page; with ``amax`` over the run's rows (fp32, NaN left out), a run from row 0 sets
 ``scale = amax / 448`` (1 if 0), one from row ``r > 0`` keeps the scale if ``amax <= 448 * scale`` and else sets
-``scale = amax / 448`` and requantises rows ``0..r-1`` from ``code * old``; rows are ``e4m3(x / scale)``.
+``scale = amax / 448`` and requantises rows ``0..r-1`` from ``code * old``; rows are ``e4m3(x / scale)``, other
+codes stay.
 """
 import numpy as np
 
@@ -19,16 +20,16 @@ def _encode(x):
     return np.where(nan, np.where(np.signbit(x), 0xFE, 0x7E), codes).astype(np.uint8)
 
 
-def _runs(slots, ps):
-    """(first entry, rows) of every run of a list of (entry, slot)."""
+def _runs(live, ps):
+    """Every run of a list of (entry, slot): its entries and its slots."""
     runs = []
-    for i, slot in slots:
-        if runs and runs[-1][0] + runs[-1][1] == i and runs[-1][2] + 1 == slot and slot % ps:
-            runs[-1][1] += 1
-            runs[-1][2] = slot
+    for i, slot in live:
+        if runs and runs[-1][1][-1] < slot and runs[-1][1][-1] // ps == slot // ps:
+            runs[-1][0].append(i)
+            runs[-1][1].append(slot)
         else:
-            runs.append([i, 1, slot])
-    return [(i, n) for i, n, _ in runs]
+            runs.append(([i], [slot]))
+    return runs
 
 
 def kv_write_slots(*, k_pages, v_pages, k_scale, v_scale, kv_dtype, page_size, slot_map, k_new, v_new,
@@ -40,13 +41,14 @@ def kv_write_slots(*, k_pages, v_pages, k_scale, v_scale, kv_dtype, page_size, s
     src = np.arange(len(slot_map)) if src_rows is None else np.asarray(src_rows)
     live = [(i, int(x)) for i, x in enumerate(slot_map)
             if 0 <= x < num_pages * page_size and 0 <= src[i] < len(k_new)]
-    for i, n in _runs(live, page_size):
-        page, r = divmod(int(slot_map[i]), page_size)
+    for entries, slots in _runs(live, page_size):
+        page, r = divmod(slots[0], page_size)
+        at = [x % page_size for x in slots]
         for pool, scale, new in ((pools[0], scales[0], k_new), (pools[1], scales[1], v_new)):
-            rows = np.asarray(new)[src[i:i + n]]
+            rows = np.asarray(new)[src[entries]]
             for h in range(hkv):
                 if kv_dtype == "bf16":
-                    pool[page, h, r:r + n] = rows[:, h]
+                    pool[page, h, at] = rows[:, h]
                     continue
                 with np.errstate(invalid="ignore"):
                     x = bf16_to_f32(rows[:, h])
@@ -59,7 +61,7 @@ def kv_write_slots(*, k_pages, v_pages, k_scale, v_scale, kv_dtype, page_size, s
                         now = amax / _F448
                         before = e4m3_to_f64(pool[page, h, :r]).astype(np.float32) * old
                         pool[page, h, :r] = _encode(before / now)
-                    pool[page, h, r:r + n] = _encode(x / now)
+                    pool[page, h, at] = _encode(x / now)
                 scale[page, h] = now
     return pools[0], pools[1], scales[0], scales[1]
 

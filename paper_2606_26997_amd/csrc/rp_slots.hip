@@ -3,8 +3,9 @@
 // rp_kv_write_slots: row i of a list goes to slot page * 16 + row. bf16 pools
 // copy. fp8 pools keep one scale per (page, kv-head) for K and for V, so the
 // entries of a page are handled together: a run is a maximal stretch of the
-// list whose slots follow each other inside one page, and one wave takes a run
-// of one kv-head's K or V: amax over the run's rows, one scale, one rounding.
+// list, skipped entries left out, whose slots rise inside one page, and one wave
+// takes a run of one kv-head's K or V: amax over the run's rows, one scale, one
+// rounding.
 //
 // rp_page_tables_resize: two exclusive prefix sums over the sequences (pages
 // given back, pages taken) say where each page of a block table goes on, or
@@ -48,6 +49,33 @@ __global__ __launch_bounds__(kWriteThreads) void write_bf16_kernel(const WriteAr
   *reinterpret_cast<uint4*>(to + (((size_t)(slot / kPage) * a.num_kv_heads + h) * kPage + slot % kPage) * D + col) = w;
 }
 
+// Entries of the list without the skipped ones between them, for a wave that
+// has some in sight: lane l holds the one before the wave's own entries (l = 0)
+// or the l-th from those on, slot -1 behind the last; returns how many of the
+// wave's own there are. In: entry first - 1 + lane, `live` and `own` as lane
+// masks. The entry before is looked for among 64, those behind the wave's own
+// among at least 64 for each: whatever a run of entries less than 64 places apart
+// needs. Two more loads, which run beside the first.
+__device__ inline int close_up(const WriteArgs& a, long long first, unsigned long long live, unsigned long long own,
+                               int2 (&line)[64], int& slot, int& src) {
+  const int lane = threadIdx.x;
+  const long long back = first - 64 + lane, ahead = first + 63 + lane;
+  int2 x = make_int2(-1, 0), y = x;
+  const bool before = back >= 0 && entry(a, back, x.x, x.y);
+  const bool behind = ahead < a.num_tokens && entry(a, ahead, y.x, y.y);
+  const unsigned long long b = __ballot(before), c = __ballot(behind), lower = (1ull << lane) - 1, mine = live & ~1ull;
+  line[lane] = make_int2(-1, 0);
+  __syncthreads();
+  if (mine >> lane & 1) line[1 + __popcll(mine & lower)] = make_int2(slot, src);
+  const int at = 1 + __popcll(mine) + __popcll(c & lower);
+  if (behind && at < 64) line[at] = y;
+  if (before && (b & ~lower) >> 1 >> lane == 0) line[0] = x;
+  __syncthreads();
+  slot = line[lane].x;
+  src = line[lane].y;
+  return __popcll(live & own);
+}
+
 // One wave: the runs that begin in `chunk` entries of the list, K or V of one
 // kv-head. D / 8 lanes hold a row, 8 values each. Whole pages are bound by
 // memory: 32 prompts of 2048 to 4096 tokens (Hkv 8, d 128) 604 MB in 119 us,
@@ -59,15 +87,21 @@ __global__ __launch_bounds__(64) void write_fp8_kernel(const WriteArgs a) {
   const int lane = threadIdx.x, Hkv = a.num_kv_heads;
   const int hv = blockIdx.x % (2 * Hkv), h = hv >> 1, v = hv & 1;
   const long long first = (long long)(blockIdx.x / (2 * Hkv)) * a.chunk;
+  __shared__ int2 line[64];
   // Lane l holds entry first - 1 + l: the one before the chunk, the chunk, and
   // the 15 that a run from its last entry can reach.
   const long long mine = first - 1 + lane;
   int slot = -1, src = 0;
-  const bool ok = mine >= 0 && mine < a.num_tokens && entry(a, mine, slot, src);
-  const int before = __shfl_up(ok ? slot : -2, 1);
-  const unsigned long long goes_on = __ballot(ok && lane > 0 && slot % kPage != 0 && before == slot - 1);
-  const unsigned long long window = (2ull << a.chunk) - 2;  // the chunk's own entries
-  unsigned long long heads = __ballot(ok) & ~goes_on & window;
+  const bool listed = mine >= 0 && mine < a.num_tokens;
+  if (listed && !entry(a, mine, slot, src)) slot = -1;
+  const unsigned long long live = __ballot(slot >= 0);
+  unsigned long long own = (2ull << a.chunk) - 2;  // the chunk's entries
+  if ((live & own) == 0) return;
+  if (live != __ballot(listed)) own = (2ull << close_up(a, first, live, own, line, slot, src)) - 2;
+  const int before = __shfl_up(slot, 1);
+  const unsigned long long goes_on =
+      __ballot(lane > 0 && before >= 0 && before / kPage == slot / kPage && before < slot);
+  unsigned long long heads = __ballot(slot >= 0) & ~goes_on & own;
   const uint16_t* from = static_cast<const uint16_t*>(v ? a.v_new : a.k_new);
   uint8_t* to = static_cast<uint8_t*>(v ? a.v_pages : a.k_pages);
   float* scales = v ? a.v_scale : a.k_scale;
@@ -80,10 +114,12 @@ __global__ __launch_bounds__(64) void write_fp8_kernel(const WriteArgs a) {
     const size_t block = (size_t)(slot0 / kPage) * Hkv + h;
     const float old = scales[block];
     uint4 w[LOADS];
+    int to_row[LOADS];
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       const int i = j * RPL + lane / LPR;
       const int row = __shfl(src, min(at + i, 63));
+      to_row[j] = __shfl(slot, min(at + i, 63)) % kPage;
       w[j] = make_uint4(0, 0, 0, 0);
       if (i < n) w[j] = *reinterpret_cast<const uint4*>(from + ((size_t)row * Hkv + h) * D + lane % LPR * 8);
     }
@@ -120,7 +156,7 @@ __global__ __launch_bounds__(64) void write_fp8_kernel(const WriteArgs a) {
       uint32_t codes[2];
       if (i < n) {
         e4m3_quotients(x[j], job.scale, inv, scaled, codes);
-        *reinterpret_cast<uint2*>(job.blk + (size_t)(r0 + i) * D + lane % LPR * 8) = make_uint2(codes[0], codes[1]);
+        *reinterpret_cast<uint2*>(job.blk + (size_t)to_row[j] * D + lane % LPR * 8) = make_uint2(codes[0], codes[1]);
       }
     }
     if (lane == 0 && (r0 == 0 || job.rows > 0)) scales[block] = job.scale;
