@@ -348,10 +348,20 @@ def draft_tree(draft_offs, masks, *, max_drafts, num_drafts=None) -> RpDraftTree
     T = int(masks.shape[0]) if num_drafts is None else int(num_drafts)
     if not isinstance(masks, int) and T > masks.shape[0]:
         raise ValueError(f"num_drafts {T}, but masks has {masks.shape[0]} entries")
-    return _holding(RpDraftTree(T, int(max_drafts), _ptr(draft_offs), _ptr(masks)), draft_offs, masks)
+    tree = _holding(RpDraftTree(T, int(max_drafts), _ptr(draft_offs), _ptr(masks)), draft_offs, masks)
+    tree.offsets = None if isinstance(draft_offs, int) else int(draft_offs.shape[0])
+    return tree
+
+
+def _fits(layout, tree) -> None:
+    """Refuse offsets of fewer sequences than the layout's: the kernels read layout.num_seqs + 1 of them."""
+    n = getattr(tree, "offsets", None)
+    if n is not None and n < layout.num_seqs + 1:
+        raise ValueError(f"draft_offs has {n} entries, {layout.num_seqs} sequences need {layout.num_seqs + 1}")
 
 
 def group_tree_attn_workspace_size(kv, layout, tree) -> int:
+    _fits(layout, tree)
     n = ctypes.c_size_t(0)
     _check(load().rp_group_tree_attn_workspace_size(ctypes.byref(kv), ctypes.byref(layout), ctypes.byref(tree),
                                                     ctypes.byref(n)), "rp_group_tree_attn_workspace_size")
@@ -361,6 +371,7 @@ def group_tree_attn_workspace_size(kv, layout, tree) -> int:
 def group_tree_attn(kv, layout, tree, q, k_draft, v_draft, softmax_scale, out, lse, workspace, stream=None) -> None:
     """Attention of every drafted token over the cache and its tree: q, out bf16 [T][Hq][d], k_draft, v_draft
     bf16 [T][Hkv][d], lse fp32 [T][Hq] or None, workspace uint8 (None where its size is 0)."""
+    _fits(layout, tree)
     T, hq, hkv, d = tree.num_drafts, layout.num_q_heads, kv.num_kv_heads, kv.head_dim
     bf16 = torch.bfloat16
     _tensors(("q", q, bf16, (T, hq, d)), ("k_draft", k_draft, bf16, (T, hkv, d)), ("v_draft", v_draft, bf16, (T, hkv, d)),
