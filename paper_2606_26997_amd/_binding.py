@@ -397,6 +397,8 @@ def page_tables_resize(tables, old_lens, new_lens, status, slot_offs=None, slot_
     S, i32 = tables.num_seqs, torch.int32
     _tensors(("old_lens", old_lens, i32, (S,)), ("new_lens", new_lens, i32, (S,)), ("status", status, i32, (4,)),
              ("slot_offs", slot_offs, i32, (S + 1,)), ("slot_map", slot_map, i32, (None,)))
+    if slot_map is not None and slot_offs is None:
+        raise RpError(RP_ERR_INVALID_ARG, "rp_page_tables_resize", "slot_map needs slot_offs")
     slots = 0 if slot_map is None else int(slot_map.shape[0])
     # An empty tensor has no address; the library then only counts against its size.
     where = (_ptr(slot_map) or _ptr(slot_offs)) if slot_map is not None else None

@@ -36,3 +36,12 @@ def test_offsets_given_by_address_are_the_caller_s(any_device):
     _calls(_layout(), rp.draft_tree(A, torch.ones(8, dtype=torch.int64), max_drafts=4))
     _calls(_layout(), rp.draft_tree(A, A, max_drafts=4, num_drafts=8))
     _calls(_layout(), B.RpDraftTree(8, 4, A, A))
+
+
+@pytest.mark.parametrize("slots", [0, 4])
+def test_slots_without_offsets(any_device, slots):
+    """Also where the slots' tensor is empty and so has no address: new tokens count against its size."""
+    tables = B.RpPageTables(2, 4, 16, 8, A, A, A)
+    with pytest.raises(rp.RpError, match="slot_map needs slot_offs") as e:
+        rp.page_tables_resize(tables, A, A, A, None, torch.zeros(slots, dtype=torch.int32))
+    assert e.value.status == rp.RP_ERR_INVALID_ARG
