@@ -353,11 +353,10 @@ __device__ void tell(const TableArgs& a, const Sums& m, int status, const long l
 // slots, 3.8 us for 16 sequences and 136 new tokens. The slots come from what the
 // tables hold before, with new pages by their rank, in the shadow of the first
 // moves' loads.
-template <class Sum>
 __global__ __launch_bounds__(1024) void tables_one_kernel(const TableArgs a) {
   __shared__ Sums m;
   long long total[3];
-  const int status = sum_up<Sum>(a, m, total);
+  const int status = sum_up<int>(a, m, total);  // of at most 8192 pages
   const bool done = status == RP_TABLES_OK;
   const auto slots = [&]() {
     if (a.slot_map != nullptr) {
@@ -406,12 +405,6 @@ __global__ __launch_bounds__(1024) void tables_slots_kernel(const TableArgs a) {
               [&](int s, int p) { return a.block_table[(size_t)s * a.max_pages + p]; });
 }
 
-template <class Sum>
-void tables_launch(const TableArgs& a, int blocks, int threads, hipStream_t stream) {
-  if (blocks == 1) tables_one_kernel<Sum><<<1, threads, 0, stream>>>(a);
-  else tables_pages_kernel<Sum><<<blocks, threads, 0, stream>>>(a);
-}
-
 }  // namespace
 
 hipError_t launch_write_slots(const WriteArgs& a, int head_dim, bool fp8, hipStream_t stream) {
@@ -441,9 +434,9 @@ hipError_t launch_page_tables(const TableArgs& a, hipStream_t stream) {
   const long long entries = (long long)a.num_seqs * a.max_pages, work = std::max<long long>(a.max_slots, entries);
   const int blocks = work <= 8192 ? 1 : (int)std::min(std::max(2ll, work / 1024), 256ll);
   const int threads = blocks > 1 || a.max_slots > 1024 || a.num_seqs > 256 ? 1024 : 256;
-  const bool wide = entries * kPage >= (1ll << 31);
-  if (wide) tables_launch<long long>(a, blocks, threads, stream);
-  else tables_launch<int>(a, blocks, threads, stream);
+  if (blocks == 1) tables_one_kernel<<<1, threads, 0, stream>>>(a);
+  else if (entries * kPage < (1ll << 31)) tables_pages_kernel<int><<<blocks, threads, 0, stream>>>(a);
+  else tables_pages_kernel<long long><<<blocks, threads, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || blocks == 1) return e;
   tables_slots_kernel<<<blocks, threads, 0, stream>>>(a);
