@@ -326,7 +326,8 @@ typedef enum {
  * All or nothing: status (int32 [4], device) gets {rp_tables_status, N, F, new
  * tokens}; unless status[0] is RP_TABLES_OK no page moves, slot_offs is 0 and
  * slot_map -1. The entries of live table rows and of the stack are the caller's
- * and not checked: a page that they hold twice is handed out twice. */
+ * and not checked: a page that they hold twice is handed out twice. Calls on one
+ * stack must not run at the same time. */
 rp_status rp_page_tables_resize(const rp_page_tables* tables, const int32_t* old_lens, const int32_t* new_lens,
                                 int32_t* status, int32_t* slot_offs, int32_t* slot_map, int32_t max_slots,
                                 hipStream_t stream);

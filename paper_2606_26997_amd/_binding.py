@@ -342,7 +342,8 @@ def _tensors(*specs) -> None:
 
 def draft_tree(draft_offs, masks, *, max_drafts, num_drafts=None) -> RpDraftTree:
     """Describe packed trees: sequence s has the drafts draft_offs[s] .. draft_offs[s+1]-1 (int32 [S + 1]),
-    masks (int64 or uint64 [T]) say which drafts of its sequence each one sees, bit u for the u-th."""
+    masks (int64 or uint64 [T]) say which drafts of its sequence each one sees, bit u for the u-th. Offsets of more
+    sequences than a layout's may be used with it."""
     _tensors(("draft_offs", draft_offs, torch.int32, (None,)),
              ("masks", masks, torch.uint64 if getattr(masks, "dtype", None) is torch.uint64 else torch.int64, (None,)))
     T = int(masks.shape[0]) if num_drafts is None else int(num_drafts)
@@ -408,7 +409,8 @@ def page_tables_resize(tables, old_lens, new_lens, status, slot_offs=None, slot_
 
 def kv_write_slots(kv, slot_map, k_new, v_new, src_rows=None, stream=None) -> None:
     """Write rows of k_new and v_new (bf16 [num_src][Hkv][d]) into the slots of slot_map (int32 [T]): row
-    src_rows[i] (int32 [T]; row i where None) into slot_map[i]; negative slots are skipped."""
+    src_rows[i] (int32 [T]; row i where None) into slot_map[i]; negative slots are skipped. fp8: the entries of a
+    page follow each other, fewer than 64 places apart, with rising slots."""
     T, rows = int(slot_map.shape[0]), int(k_new.shape[0])
     row = (rows, kv.num_kv_heads, kv.head_dim)
     _tensors(("slot_map", slot_map, torch.int32, (T,)), ("k_new", k_new, torch.bfloat16, row),

@@ -114,7 +114,8 @@ class DeviceBatch:
                           self.softmax_scale, self.draft_out, self.draft_lse, self.draft_workspace, stream)
 
     def write_slots(self, slot_map, k_new, v_new, src_rows=None, stream=None):
-        """Rows of k_new and v_new into slots of the batch's pool (accepted drafts, say)."""
+        """Rows of k_new and v_new into slots of the batch's pool: accepted drafts, say, gathered by ``src_rows`` or
+        in place with -1 for the others."""
         B.kv_write_slots(self.kv, slot_map, k_new, v_new, src_rows, stream)
 
     # -- decode step from the raw projections ---------------------------------
@@ -179,7 +180,8 @@ class DeviceBatch:
 
 class PageTables:
     """Block tables of up to ``num_seqs`` sequences (or prefixes) on the device, their lengths, and the stack of
-    a pool's free pages. Tables of one pool share its stack: pass ``stack`` of the first one to the others."""
+    a pool's free pages. Tables of one pool share its stack: pass ``stack`` of the first one to the others, and do
+    not resize two of them at the same time."""
 
     def __init__(self, *, num_seqs, max_pages, num_pages=None, stack=None, device="cuda"):
         d = torch.device(device)

@@ -27,9 +27,10 @@ struct KeyStage {
 };
 
 // One direct global-to-LDS copy by a whole wave: 16 bytes per lane from
-// base + off (or from the lane's own address) to lds + 16 * lane. Written in assembly because the compiler waits for every
-// load in flight before any LDS read that follows its own form of it;
-// wait_copies waits for as many as are needed.
+// base + off (or from the lane's own address) to lds + 16 * lane. Written in
+// assembly because the compiler waits for every load in flight before any LDS
+// read that follows its own form of it; wait_copies waits for as many as are
+// needed.
 __device__ inline void copy_to_lds(uint32_t lds, const uint16_t* base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :

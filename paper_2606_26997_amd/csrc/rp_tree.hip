@@ -526,7 +526,7 @@ __device__ __forceinline__ void walk(const TreeArgs& a, const Keys& k, int h, in
 }
 
 // A unit: the columns in sm.row over `k`, split between the waves, merged and
-// stored: final rows (slot < 0), or the partial results in their slot.
+// stored: as final rows (part == kFinal), or as partial results from `part` on.
 template <int D, bool FP8, int CT>
 __device__ __forceinline__ void split_unit(const TreeArgs& a, const Keys& k, int h, long long part,
                                            Smem<D, FP8, CT>& sm) {
@@ -1258,9 +1258,11 @@ __device__ inline unsigned long long column_mask(const TreeArgs& a, const SeqUni
 // Bound by the reads of the cache: 256 sequences of 8 drafts over 64 to 512 +
 // U[0, 4096] tokens (Hkv 8, d 128) 2.21 GB in 380 us, 5.8 TB/s, of the 7.0 that
 // one large read reaches; 64 fp8 sequences of 1 to 32 drafts over 8192 to 32768
-// tokens 2.70 GB in 540 to 590 us, 4.6 to 5.0 TB/s, where decoding and the
-// softmax of four tiles take as long as the reads. Small calls are latency: lengths, then page
-// ids, then pages, 7 us for 4 sequences of 180 tokens.
+// tokens 2.70 GB in 540 to 590 us, 4.6 to 5.0 TB/s, with decoding and the softmax
+// of four tiles between the reads (vector units 42% busy, matrix units 19%). Four
+// tiles of 128-wide heads take all 256 registers and spill 28 bytes a lane (fp8:
+// 12). Small calls are latency: lengths, then page ids, then pages, 7 us for 4
+// sequences of 180 tokens.
 template <int D, bool FP8, int CT>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
 void tree_split_kernel(const TreeArgs a) {
@@ -1295,9 +1297,12 @@ void tree_split_kernel(const TreeArgs a) {
   else take(sm.split);
 }
 
-// Bound by the matrix products and the softmax between them: 32 sequences of 64
-// drafts with 8 query heads per kv-head over 1024 + U[0, 2048] tokens (Hkv 4, d
-// 128) 69 GFLOP in 105 us, 660 TFLOP/s, of the 1170 of a large product.
+// Bound by the chain of scores, softmax and products that each wave waits for, with
+// two waves per SIMD (236 registers): 32 sequences of 64 drafts with 8 query heads
+// per kv-head over 1024 + U[0, 2048] tokens (Hkv 4, d 128) 69 GFLOP in 103 to 105
+// us among others of their kind, 660 TFLOP/s, of the 1170 to 1220 of a large
+// product, and 117 to 121 apart under a kernel trace; matrix units 25% busy, vector
+// units 30%.
 template <int D, bool FP8, int RT>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
 void tree_rows_kernel(const TreeArgs a) {
