@@ -55,7 +55,8 @@ __global__ __launch_bounds__(kWriteThreads) void write_bf16_kernel(const WriteAr
 // wave's own there are. In: entry first - 1 + lane, `live` and `own` as lane
 // masks. The entry before is looked for among 64, those behind the wave's own
 // among at least 64 for each: whatever a run of entries less than 64 places apart
-// needs. Two more loads, which run beside the first.
+// needs. Two more loads, side by side (256 sequences of 8 drafts, half of them
+// accepted, Hkv 8, d 128: in place 11.0 us, gathered to half the entries 10.0).
 __device__ inline int close_up(const WriteArgs& a, long long first, unsigned long long live, unsigned long long own,
                                int2 (&line)[64], int& slot, int& src) {
   const int lane = threadIdx.x;
