@@ -468,6 +468,144 @@ rp_status rp_plan_layout(const rp_paged_kv* kv, const rp_group_layout* layout, r
 rp_status rp_validate_layout(const rp_paged_kv* kv, const rp_group_layout* layout,
                              hipStream_t stream);
 
+/* ---- Rows of logits ------------------------------------------------------
+ * What a rollout does with its model's outputs and training does with them
+ * again: a token is drawn from each row (the decode workers, paper Section 4),
+ * its log-probability is kept, and the group's advantages (Eq. 1, below) enter
+ * a loss whose gradient goes back into the rows.
+ *
+ * Row n holds `vocab` logits x of one token position. At temperature T,
+ *   p_i = exp(x_i / T) / sum_j exp(x_j / T),  H = - sum_i p_i ln p_i.
+ * A logit of -inf is a token that cannot occur. A row without a finite logit
+ * is empty: token -1, log-probability -inf, entropy, loss and gradient 0. A NaN
+ * or +inf among a row's logits makes its token -1 and its other results NaN. */
+typedef enum {
+  RP_LOGITS_BF16 = 0,
+  RP_LOGITS_F16 = 1,
+  RP_LOGITS_F32 = 2
+} rp_logits_dtype;
+
+typedef struct {
+  const void* data;      /* row n begins n * row_stride elements behind data; aligned to its element */
+  int32_t num_rows;
+  int32_t vocab;         /* 1 .. 1048576 */
+  int64_t row_stride;    /* elements, >= vocab; what lies between rows is neither read nor written */
+  rp_logits_dtype dtype;
+} rp_logits;
+
+/* Workspace bytes that any of the calls below needs for this shape (0 for
+ * many). Depends on host-side scalars only; *bytes is a host pointer. The
+ * workspace is a device buffer, 256-byte aligned, and may be NULL where the
+ * size is 0; concurrent calls need distinct workspaces. */
+rp_status rp_logits_workspace_size(const rp_logits* logits, size_t* bytes);
+
+/* How each row is sampled: device arrays of num_rows entries, any of them NULL.
+ * The vocabulary is sorted by logit, the lowest index first among equals; the
+ * tokens kept are the first min(n_k, n_p, n_m), at least one:
+ *   temperature T (NULL: 1): weights w_i = exp((x_i - max x) / T). T <= 0 (or
+ *     NaN) is greedy: the largest logit of the lowest index is taken.
+ *   top_k (NULL or <= 0: all): n_k = min(top_k, vocab).
+ *   top_p (NULL, NaN or >= 1: all): n_p is the least n with
+ *     w_1 + .. + w_n >= top_p (w_1 + .. + w_{n_k}).
+ *   min_p (NULL, NaN or <= 0: all; above 1 as 1): n_m counts the w_i >= min_p. */
+typedef struct {
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+} rp_sampling;
+
+/* Draw a token from every row: with W the weights' sum over the kept tokens,
+ * the least index i such that the weights of the kept tokens 0 .. i sum to
+ * more than u[n] W (u: fp32 [num_rows], in [0, 1); values outside are taken
+ * for the nearest inside, NaN for 0). Weights and their sums are held in 64
+ * bits: the token is that of exact arithmetic unless u W lies within about
+ * 1e-12 W of a border (a step of u is 6e-8).
+ * tokens: int32 [num_rows]. logprobs (fp32 [num_rows], or NULL): ln of the
+ * token's probability in the whole row at T (at 1 where T is greedy), what
+ * rp_token_logprobs gives. kept_logprobs (the same): ln of its probability
+ * among the kept tokens, with which it was drawn (0 where greedy).
+ * sampling may be NULL (all tokens, T = 1). */
+rp_status rp_sample_tokens(const rp_logits* logits, const rp_sampling* sampling, const float* u,
+                           int32_t* tokens, float* logprobs, float* kept_logprobs,
+                           void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ln p of given tokens (int32 [num_rows]) and the rows' entropies, at one
+ * temperature (finite, > 0): logprobs fp32 [num_rows]; entropy fp32 [num_rows]
+ * or NULL. A row whose token is outside [0, vocab) is skipped: both are 0. */
+rp_status rp_token_logprobs(const rp_logits* logits, const int32_t* tokens, double temperature,
+                            float* logprobs, float* entropy,
+                            void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* GRPO's clipped policy loss (the training that Section 4's trainer does with
+ * Eq. 1's advantages). For row n with token y, l = ln p_y at `temperature`,
+ * A = advantages[row_seq[n]] (advantages[n] where row_seq is NULL):
+ *   r = exp(l - old_logprobs[n]),  s = min(r A, clip(r, 1 - clip_low, 1 + clip_high) A),
+ *   k = exp(ref - l) - (ref - l) - 1 with ref = ref_logprobs[n],
+ *   losses[n] = weights[n] (- s + kl_beta k - entropy_coef H).
+ * Rows whose token is outside [0, vocab), or whose row_seq is outside
+ * [0, num_advantages), are skipped: their logits are not read, and loss,
+ * log-probability, entropy and gradient are 0. A weight of 0 gives loss and
+ * gradient 0 whatever else the row holds. */
+typedef struct {
+  const int32_t* tokens;        /* [num_rows] */
+  const float* old_logprobs;    /* [num_rows], of the policy that drew the tokens */
+  const float* ref_logprobs;    /* [num_rows]; may be NULL where kl_beta is 0 */
+  const float* advantages;      /* [num_advantages], per sequence or per row */
+  const int32_t* row_seq;       /* [num_rows] or NULL */
+  int32_t num_advantages;       /* >= num_rows where row_seq is NULL */
+  const float* weights;         /* [num_rows] or NULL (1) */
+  double temperature;           /* finite, > 0 */
+  double clip_low, clip_high;   /* >= 0 and not NaN; clip_high may be infinite */
+  double kl_beta, entropy_coef; /* finite; 0 leaves the term out */
+} rp_policy_batch;
+
+/* Losses, and the gradient of their sum: dlogits[n][i] = d losses[n] / d x_i,
+ * rows dlogits_stride elements apart, in the logits' type, rounded once; NULL
+ * for the losses alone. dlogits may be the logits themselves (same stride),
+ * and must not overlap them otherwise. At a border of the clip the gradient is
+ * the unclipped side's. losses, logprobs (l), entropy (H): fp32 [num_rows],
+ * the latter two may be NULL. */
+rp_status rp_policy_loss(const rp_logits* logits, const rp_policy_batch* batch,
+                         float* losses, float* logprobs, float* entropy,
+                         void* dlogits, int64_t dlogits_stride,
+                         void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Distillation from a teacher that gives its likeliest tokens only: row n
+ * lists ids[n][j] with values[n][j], j < k. Entries outside [0, vocab), entries
+ * whose value is -inf, and ids that the row lists before do not count. With q
+ * the student's probabilities at `temperature`, over the entries that count:
+ *   RP_DISTILL_TOPK: values are the teacher's logits (or log-probabilities),
+ *     P = softmax(values / temperature) over the list, loss = sum P (ln P - ln q).
+ *   RP_DISTILL_TAIL: values are log-probabilities at `temperature`, P =
+ *     exp(values); what is outside the list is one more class, with
+ *     P_o = max(1 - sum P, 2^-24) and q_o = the student's mass outside the list:
+ *     loss = sum P (ln P - ln q) + P_o (ln P_o - ln q_o).
+ *   RP_DISTILL_REVERSE: the same classes,
+ *     loss = sum q (ln q - ln P) + q_o (ln q_o - ln P_o).
+ * A class outside to which the student gives nothing (every other token masked)
+ * is left out. */
+typedef enum {
+  RP_DISTILL_TOPK = 0,
+  RP_DISTILL_TAIL = 1,
+  RP_DISTILL_REVERSE = 2
+} rp_distill_kind;
+
+typedef struct {
+  const int32_t* ids;     /* [num_rows][k] */
+  const float* values;    /* [num_rows][k] */
+  int32_t k;              /* 1 .. 1024 */
+  rp_distill_kind kind;
+  const float* weights;   /* [num_rows] or NULL (1); rows of weight 0 are not read: loss and gradient 0 */
+  double temperature;     /* finite, > 0 */
+} rp_teacher;
+
+/* losses[n] = weights[n] loss (fp32 [num_rows]) and the gradient of their sum;
+ * dlogits as in rp_policy_loss. */
+rp_status rp_distill_loss(const rp_logits* logits, const rp_teacher* teacher, float* losses,
+                          void* dlogits, int64_t dlogits_stride,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* ---- GRPO group statistics (Eq. 1) -----------------------------------
  * For each of num_groups groups of group_size rewards r_1..r_K (fp32,
  * rewards[g][i], device), in fp64:

@@ -35,10 +35,12 @@ from .qkprep import decode_positions, decode_step_prep, qk_prep, rms_norm, rope
 from .sched import simulate as simulate_schedule
 from .slots import kv_write_slots, page_tables_resize
 from .tree import tree_attention, tree_for_workload
+from .rows import distill_loss, kept_tokens, policy_loss, sample, token_logprobs
 from .grpo import advantage, advantage_f32, group_stats
 
 __all__ = ["bf16_to_f64", "bf16_to_f32", "e4m3_to_f64", "e4m3_encode", "E4M3_MAX",
            "decode_attention", "key_slots", "attention_for_workload",
            "lse_combine", "kv_append", "append_for_workload", "prefill_attention", "prefill_kv_write",
            "decode_positions", "decode_step_prep", "qk_prep", "rms_norm", "rope",
-           "kv_write_slots", "page_tables_resize", "tree_attention", "tree_for_workload", "simulate_schedule", "advantage", "advantage_f32", "group_stats"]
+           "kv_write_slots", "page_tables_resize", "tree_attention", "tree_for_workload", "simulate_schedule", "advantage", "advantage_f32", "group_stats",
+           "distill_loss", "kept_tokens", "policy_loss", "sample", "token_logprobs"]

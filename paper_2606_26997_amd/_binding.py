@@ -32,7 +32,11 @@ EXPORTED = ("rp_status_string", "rp_last_error", "rp_kv_append",
             "rp_prefill_kv_write", "rp_prefill_attn", "rp_decode_qk_prep", "rp_sched_simulate",
             "rp_grpo_advantage", "rp_prefill", "rp_group_decode_attn_noalloc", "rp_decode_qk_prep_plan",
             "rp_selftest_mfma", "rp_stream_read", "rp_group_tree_attn_workspace_size", "rp_group_tree_attn",
-            "rp_kv_write_slots", "rp_page_tables_resize")
+            "rp_kv_write_slots", "rp_page_tables_resize", "rp_logits_workspace_size", "rp_sample_tokens",
+            "rp_token_logprobs", "rp_policy_loss", "rp_distill_loss")
+# include/rp.h rp_logits_dtype and rp_distill_kind
+RP_LOGITS_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+RP_DISTILL_KINDS = {"topk": 0, "tail": 1, "reverse": 2}
 # include/rp.h rp_tables_status, as the device's status[0] holds it
 RP_TABLES_OK, RP_TABLES_NO_PAGES, RP_TABLES_BAD_LENGTH, RP_TABLES_NO_SLOTS, RP_TABLES_BAD_FREE_LIST = range(5)
 RP_STREAM_READ_SINK_WORDS = 2048 * 4   # include/rp.h
@@ -73,6 +77,26 @@ class RpPageTables(ctypes.Structure):
     _fields_ = [("num_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("num_pages", ctypes.c_int32), ("block_table", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
                 ("free_count", ctypes.c_void_p)]
+
+
+class RpLogits(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("num_rows", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("row_stride", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class RpSampling(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")]
+
+
+class RpPolicyBatch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("tokens", "old_logprobs", "ref_logprobs", "advantages", "row_seq")] + \
+               [("num_advantages", ctypes.c_int32), ("weights", ctypes.c_void_p)] + \
+               [(n, ctypes.c_double) for n in ("temperature", "clip_low", "clip_high", "kl_beta", "entropy_coef")]
+
+
+class RpTeacher(ctypes.Structure):
+    _fields_ = [("ids", ctypes.c_void_p), ("values", ctypes.c_void_p), ("k", ctypes.c_int32), ("kind", ctypes.c_int32),
+                ("weights", ctypes.c_void_p), ("temperature", ctypes.c_double)]
 
 
 class RpPlanInfo(ctypes.Structure):
@@ -140,6 +164,11 @@ def load() -> ctypes.CDLL:
         "rp_group_tree_attn": (ctypes.c_int, [P, P, P, P, P, P, F32, P, P, P, ctypes.c_size_t, P]),
         "rp_kv_write_slots": (ctypes.c_int, [P, P, I32, P, P, P, I32, P]),
         "rp_page_tables_resize": (ctypes.c_int, [P, P, P, P, P, P, I32, P]),
+        "rp_logits_workspace_size": (ctypes.c_int, [P, ctypes.POINTER(ctypes.c_size_t)]),
+        "rp_sample_tokens": (ctypes.c_int, [P, P, P, P, P, P, P, ctypes.c_size_t, P]),
+        "rp_token_logprobs": (ctypes.c_int, [P, P, ctypes.c_double, P, P, P, ctypes.c_size_t, P]),
+        "rp_policy_loss": (ctypes.c_int, [P, P, P, P, P, P, ctypes.c_int64, P, ctypes.c_size_t, P]),
+        "rp_distill_loss": (ctypes.c_int, [P, P, P, P, ctypes.c_int64, P, ctypes.c_size_t, P]),
         "rp_stream_read": (ctypes.c_int, [P, ctypes.c_uint64, P, I32, P]),
     }
     for name, (res, args) in sig.items():
@@ -417,6 +446,105 @@ def kv_write_slots(kv, slot_map, k_new, v_new, src_rows=None, stream=None) -> No
              ("v_new", v_new, torch.bfloat16, row), ("src_rows", src_rows, torch.int32, (T,)))
     _check(load().rp_kv_write_slots(ctypes.byref(kv), _ptr(slot_map), T, _ptr(k_new), _ptr(v_new), _ptr(src_rows),
                                     rows, _stream(stream)), "rp_kv_write_slots")
+
+
+def _rows(name, t, like=None):
+    """(rows, vocab, stride) of a [rows][vocab] tensor whose rows are contiguous; `like`: of that one's shape, dtype
+    and device."""
+    if t.dtype not in RP_LOGITS_DTYPES or (like is not None and t.dtype is not like.dtype):
+        raise ValueError(f"{name}: dtype {t.dtype}, not "
+                         f"{'bfloat16, float16 or float32' if like is None else like.dtype}")
+    if t.dim() != 2 or (like is not None and t.shape != like.shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, not {'[rows][vocab]' if like is None else tuple(like.shape)}")
+    n, v = t.shape
+    if v > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the logits of a row must be contiguous (strides {t.stride()})")
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+    stride = t.stride(0) if n > 1 else v
+    if stride < v:
+        raise ValueError(f"{name}: rows overlap (strides {t.stride()})")
+    return n, v, stride
+
+
+def _logits(t) -> RpLogits:
+    n, v, stride = _rows("logits", t)
+    return RpLogits(t.data_ptr(), n, v, stride, RP_LOGITS_DTYPES[t.dtype])
+
+
+def logits_workspace_size(logits) -> int:
+    """Bytes of workspace that any of the calls on these logits ([rows][vocab], bf16, fp16 or fp32) needs."""
+    n = ctypes.c_size_t(0)
+    _check(load().rp_logits_workspace_size(ctypes.byref(_logits(logits)), ctypes.byref(n)), "rp_logits_workspace_size")
+    return int(n.value)
+
+
+def sample_tokens(logits, u, tokens, logprobs=None, kept_logprobs=None, *, temperature=None, top_k=None, top_p=None,
+                  min_p=None, workspace=None, stream=None) -> None:
+    """Draw tokens (int32 [rows]) from logits [rows][vocab] with the uniform numbers u (fp32 [rows]); logprobs and
+    kept_logprobs fp32 [rows] or None. temperature, top_p, min_p: fp32 [rows]; top_k: int32 [rows]; None for none."""
+    l, f32 = _logits(logits), torch.float32
+    row = (l.num_rows,)
+    _tensors(("u", u, f32, row), ("tokens", tokens, torch.int32, row), ("logprobs", logprobs, f32, row),
+             ("kept_logprobs", kept_logprobs, f32, row), ("temperature", temperature, f32, row),
+             ("top_k", top_k, torch.int32, row), ("top_p", top_p, f32, row), ("min_p", min_p, f32, row),
+             ("workspace", workspace, None, None))
+    how = RpSampling(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
+    _check(load().rp_sample_tokens(ctypes.byref(l), ctypes.byref(how), _ptr(u), _ptr(tokens), _ptr(logprobs),
+                                   _ptr(kept_logprobs), _ptr(workspace), _ws_bytes(workspace), _stream(stream)),
+           "rp_sample_tokens")
+
+
+def token_logprobs(logits, tokens, logprobs, entropy=None, *, temperature=1.0, workspace=None, stream=None) -> None:
+    """Log-probabilities (fp32 [rows]) of tokens (int32 [rows]; others than 0 .. vocab-1 are skipped) in logits
+    [rows][vocab], and the rows' entropies (fp32 [rows] or None)."""
+    l = _logits(logits)
+    row = (l.num_rows,)
+    _tensors(("tokens", tokens, torch.int32, row), ("logprobs", logprobs, torch.float32, row),
+             ("entropy", entropy, torch.float32, row), ("workspace", workspace, None, None))
+    _check(load().rp_token_logprobs(ctypes.byref(l), _ptr(tokens), float(temperature), _ptr(logprobs), _ptr(entropy),
+                                    _ptr(workspace), _ws_bytes(workspace), _stream(stream)), "rp_token_logprobs")
+
+
+def policy_loss(logits, tokens, old_logprobs, advantages, losses, dlogits=None, *, row_seq=None, weights=None,
+                ref_logprobs=None, logprobs=None, entropy=None, temperature=1.0, clip_low=0.2, clip_high=0.2,
+                kl_beta=0.0, entropy_coef=0.0, workspace=None, stream=None) -> None:
+    """GRPO's clipped policy loss of every row (losses fp32 [rows]) and, in dlogits (of the logits' shape and type;
+    it may be the logits), the gradient of their sum. tokens, row_seq: int32 [rows]; advantages: fp32, of any shape,
+    entry row_seq[n] for row n (n without row_seq); old_logprobs, ref_logprobs, weights, logprobs, entropy: fp32
+    [rows]. Rows whose token or row_seq is out of range are skipped."""
+    l, f32 = _logits(logits), torch.float32
+    row = (l.num_rows,)
+    _tensors(("tokens", tokens, torch.int32, row), ("old_logprobs", old_logprobs, f32, row),
+             ("advantages", advantages, f32, None), ("losses", losses, f32, row),
+             ("row_seq", row_seq, torch.int32, row), ("weights", weights, f32, row),
+             ("ref_logprobs", ref_logprobs, f32, row), ("logprobs", logprobs, f32, row),
+             ("entropy", entropy, f32, row), ("workspace", workspace, None, None))
+    stride = _rows("dlogits", dlogits, logits)[2] if dlogits is not None else 0
+    batch = RpPolicyBatch(_ptr(tokens), _ptr(old_logprobs), _ptr(ref_logprobs), _ptr(advantages), _ptr(row_seq),
+                          advantages.numel(), _ptr(weights), float(temperature), float(clip_low), float(clip_high),
+                          float(kl_beta), float(entropy_coef))
+    _check(load().rp_policy_loss(ctypes.byref(l), ctypes.byref(batch), _ptr(losses), _ptr(logprobs), _ptr(entropy),
+                                 _ptr(dlogits), stride, _ptr(workspace), _ws_bytes(workspace), _stream(stream)),
+           "rp_policy_loss")
+
+
+def distill_loss(logits, ids, values, losses, dlogits=None, *, kind="tail", weights=None, temperature=1.0,
+                 workspace=None, stream=None) -> None:
+    """Divergence of every row (losses fp32 [rows]) from a teacher's list (ids int32, values fp32 [rows][k]) and, in
+    dlogits (of the logits' shape and type; it may be the logits), the gradient of the losses' sum. kind: a key of
+    RP_DISTILL_KINDS; weights fp32 [rows] or None."""
+    if kind not in RP_DISTILL_KINDS:
+        raise ValueError(f"kind {kind!r}, not one of {', '.join(RP_DISTILL_KINDS)}")
+    l, f32 = _logits(logits), torch.float32
+    _tensors(("ids", ids, torch.int32, (l.num_rows, None)), ("values", values, f32, (l.num_rows, ids.shape[1])),
+             ("losses", losses, f32, (l.num_rows,)), ("weights", weights, f32, (l.num_rows,)),
+             ("workspace", workspace, None, None))
+    stride = _rows("dlogits", dlogits, logits)[2] if dlogits is not None else 0
+    teacher = RpTeacher(_ptr(ids), _ptr(values), ids.shape[1], RP_DISTILL_KINDS[kind], _ptr(weights),
+                        float(temperature))
+    _check(load().rp_distill_loss(ctypes.byref(l), ctypes.byref(teacher), _ptr(losses), _ptr(dlogits), stride,
+                                  _ptr(workspace), _ws_bytes(workspace), _stream(stream)), "rp_distill_loss")
 
 
 def prefill_layout(prompt_offs, prefix_block_table, *, num_q_heads, num_tokens) -> RpPrefillLayout:

@@ -13,7 +13,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "librp.so")
 SOURCES = ["rp_api.hip", "rp_plan.hip", "rp_attn.hip", "rp_combine.hip", "rp_append.hip", "rp_prefill.hip",
            "rp_qkprep.hip", "rp_grpo.hip", "rp_selftest.hip", "rp_tree.hip",
-           "rp_slots.hip"]
+           "rp_slots.hip", "rp_logits.hip", "rp_sample.hip", "rp_losses.hip"]
 # Host-only C++ (no device code), built with the system compiler.
 HOST_SOURCES = ["rp_sched.cpp"]
 ARCH = "gfx950"

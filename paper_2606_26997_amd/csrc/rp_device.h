@@ -41,6 +41,11 @@ constexpr float kLog2e = 1.4426950408889634f;
 // accumulator unscaled.
 constexpr float kLazyMax = 8.0f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr double kLog2e64 = 1.4426950408889634;
+constexpr double kLn2_64 = 0.6931471805599453;
+// Entries of a teacher's list of one row, and the largest vocabulary.
+constexpr int kMaxListed = 1024;
+constexpr int kMaxVocab = 1 << 20;
 
 // Plan header slots.
 enum : int {

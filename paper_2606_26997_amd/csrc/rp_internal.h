@@ -243,6 +243,62 @@ struct ValidateArgs {
   int* result;       // [4]: error count, first bad kind, first bad index, value
 };
 
+// Rows of logits, and what goes with each (rp.h states the meaning).
+struct LogitArgs {
+  const void* data;
+  int rows, vocab;
+  long long stride;  // elements
+};
+
+struct SampleArgs {
+  LogitArgs logits;
+  const float* temperature;
+  const int* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* u;
+  int* tokens;
+  float* logprobs;
+  float* kept;
+};
+
+struct LogprobArgs {
+  LogitArgs logits;
+  const int* tokens;
+  double inv_t;  // 1 / temperature
+  float* logprobs;
+  float* entropy;
+};
+
+struct PolicyArgs {
+  LogitArgs logits;
+  const int* tokens;
+  const float* old_logprobs;
+  const float* ref_logprobs;  // null where kl_beta is 0
+  const float* advantages;
+  const int* row_seq;
+  int num_advantages;
+  const float* weights;
+  double inv_t, clip_low, clip_high, kl_beta, entropy_coef;
+  float* losses;
+  float* logprobs;
+  float* entropy;
+  void* dlogits;
+  long long dstride;
+};
+
+struct DistillArgs {
+  LogitArgs logits;
+  const int* ids;
+  const float* values;
+  int k, kind;
+  const float* weights;
+  double inv_t;
+  float* losses;
+  void* dlogits;
+  long long dstride;
+};
+
 hipError_t launch_plan(const PlanArgs& a, hipStream_t stream);
 // q/k prep and the plan of the attention after its append in one launch
 // (batches of at most 64 sequences; the plan's len_add is 1).
@@ -267,6 +323,10 @@ hipError_t launch_prefill_kv_write(const PrefillArgs& a, int head_dim, bool fp8,
 hipError_t launch_prefill_attn(const PrefillArgs& a, int head_dim, int n_rep, hipStream_t stream);
 hipError_t launch_qk_prep(QkPrepArgs a, int head_dim, bool fp8, hipStream_t stream);
 hipError_t launch_grpo(const GrpoArgs& a, hipStream_t stream);
+hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t stream);
+hipError_t launch_logprobs(const LogprobArgs& a, int dtype, hipStream_t stream);
+hipError_t launch_policy(const PolicyArgs& a, int dtype, hipStream_t stream);
+hipError_t launch_distill(const DistillArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_validate(const ValidateArgs& a, hipStream_t stream);
 hipError_t launch_selftest_mfma(int shape, const void* a, const void* b, float* c, hipStream_t stream);
 hipError_t launch_stream_read(const void* src, uint64_t bytes, uint32_t* sink, bool nontemporal,
