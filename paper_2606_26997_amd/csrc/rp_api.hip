@@ -1081,6 +1081,7 @@ rp_status rp_stream_read(const void* src, uint64_t bytes, uint32_t* sink, int32_
 }  // extern "C"
 
 namespace rp {
+rp_status device_cus(int* cus) { return ::device_cus(cus); }
 rp_status set_error(rp_status st, const char* msg) {
   snprintf(g_err, sizeof(g_err), "%s", msg);
   return st;

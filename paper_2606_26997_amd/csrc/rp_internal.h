@@ -248,7 +248,11 @@ struct LogitArgs {
   const void* data;
   int rows, vocab;
   long long stride;  // elements
+  int num_cus;       // compute units of the device
 };
+
+// Compute units of the current device.
+rp_status device_cus(int* cus);
 
 struct SampleArgs {
   LogitArgs logits;

@@ -46,7 +46,7 @@ rp_status check_rows(const rp_logits* l, Rows* r) {
     return fail(RP_ERR_INVALID_ARG, "row_stride %lld must be in [vocab, 2^31)", (long long)l->row_stride);
   if (l->num_rows > 0 && (l->data == nullptr || !aligned(l->data, r->bytes)))
     return fail(RP_ERR_INVALID_ARG, "logits data must be non-NULL and aligned to its elements");
-  r->args = {l->data, l->num_rows, l->vocab, l->row_stride};
+  r->args = {l->data, l->num_rows, l->vocab, l->row_stride, 0};
   return RP_OK;
 }
 
@@ -161,6 +161,7 @@ rp_status rp_policy_loss(const rp_logits* logits, const rp_policy_batch* b, floa
     return fail(RP_ERR_INVALID_ARG, "ref_logprobs/advantages/row_seq/weights/logprobs/entropy must be 4-byte aligned");
   st = check_gradient(r, dlogits, dlogits_stride);
   if (st == RP_OK) st = check_workspace(workspace_need(r), workspace, workspace_bytes);
+  if (st == RP_OK) st = rp::device_cus(&r.args.num_cus);
   if (st != RP_OK) return st;
   const rp::PolicyArgs a{r.args, b->tokens, b->old_logprobs, b->kl_beta != 0.0 ? b->ref_logprobs : nullptr,
                          b->advantages, b->row_seq, b->num_advantages, b->weights, 1.0 / b->temperature, b->clip_low,
@@ -188,6 +189,7 @@ rp_status rp_distill_loss(const rp_logits* logits, const rp_teacher* t, float* l
     return fail(RP_ERR_INVALID_ARG, "ids/values/losses must be non-NULL, and with weights 4-byte aligned");
   st = check_gradient(r, dlogits, dlogits_stride);
   if (st == RP_OK) st = check_workspace(workspace_need(r), workspace, workspace_bytes);
+  if (st == RP_OK) st = rp::device_cus(&r.args.num_cus);
   if (st != RP_OK) return st;
   const rp::DistillArgs a{r.args, t->ids, t->values, t->k, kind, t->weights, 1.0 / t->temperature, losses,
                           dlogits, dlogits_stride};

@@ -69,29 +69,25 @@ __device__ inline u32x4_any pack(const float (&x)[Elem<DT>::kPerVec]) {
   return v;
 }
 
-// Vector `vec` of a row: elements vec * E .. vec * E + E - 1, those from
-// `vocab` on as -inf.
+// Vector `vec` of a row: elements vec * E .. vec * E + E - 1, all of them in the row.
+template <int DT>
+__device__ inline u32x4_any load_whole(const void* row, int vec) {
+  return *reinterpret_cast<const u32x4_any*>(static_cast<const char*>(row) + (size_t)vec * 16);
+}
+template <int DT>
+__device__ inline void store_whole(void* row, int vec, const float (&x)[Elem<DT>::kPerVec]) {
+  *reinterpret_cast<u32x4_any*>(static_cast<char*>(row) + (size_t)vec * 16) = pack<DT>(x);
+}
+// The same where the row may end inside: elements from `vocab` on are -inf.
 template <int DT>
 __device__ inline u32x4_any load_vec(const void* row, int vec, int vocab) {
   constexpr int E = Elem<DT>::kPerVec;
   const int first = vec * E;
-  if (first + E <= vocab) return *reinterpret_cast<const u32x4_any*>(static_cast<const char*>(row) + (size_t)vec * 16);
+  if (first + E <= vocab) return load_whole<DT>(row, vec);
   float x[E];
 #pragma unroll
   for (int k = 0; k < E; ++k) x[k] = first + k < vocab ? Elem<DT>::get(row, first + k) : -INFINITY;
   return pack<DT>(x);
-}
-template <int DT>
-__device__ inline void store_vec(void* row, int vec, int vocab, const float (&x)[Elem<DT>::kPerVec]) {
-  constexpr int E = Elem<DT>::kPerVec;
-  const int first = vec * E;
-  if (first + E <= vocab) {
-    *reinterpret_cast<u32x4_any*>(static_cast<char*>(row) + (size_t)vec * 16) = pack<DT>(x);
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < E; ++k)
-    if (first + k < vocab) put_elem<DT>(row, first + k, x[k]);
 }
 
 // Sums and maxima over a wave and over a workgroup of NT threads, in every

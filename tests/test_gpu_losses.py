@@ -334,3 +334,73 @@ def test_a_small_mass_outside_the_list():
     for kind in ("tail", "reverse"):
         grad, _ = guarded(2, V, "f32")
         _distill_check(x, "f32", ids, values, kind, None, 1.0, _distill_run(view, ids, values, kind, None, 1.0, grad), kind + " ")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [600, 30001, 200000])
+def test_one_token_with_nearly_all_the_mass(V, dtype):
+    """ln p of a token of probability 1 - 1e-4 and closer, the entropy and the gradient there keep their digits: the other
+    terms' sum is off by (3 |z| + 2 + V / 2048 + 16) u, with |z| below 40."""
+    import paper_2606_26997_amd as rp
+    say(f"dominant token {V} {dtype}")
+    rng = np.random.default_rng(V)
+    n = 4
+    x, view, _ = logits(rng, n, V, dtype, scale=0.5, peaks=0)
+    at = np.array([0, V - 1, V // 2, 7])
+    for r in range(n):
+        view[r, int(at[r])] = 22.0 + 3 * r
+    x = view.double().cpu().numpy()
+    rel = 3 * ((3 * 40 + 2 + V / 2048 + 16) * U)
+    lp, H = empty(n), empty(n)
+    rp.token_logprobs(view, dev(at, torch.int32), lp, H, workspace=workspace(view))
+    want = oracle.token_logprobs(x, at)
+    # The oracle's own ln(1 + small) is off by 2^-53 of 1.
+    _near(lp.double().cpu(), want[0], rel * np.abs(want[0]) + 2e-16, "logprobs")
+    _near(H.double().cpu(), want[1], 3 * rel * np.abs(want[1]) + 1e-14, "entropy")
+    case = (at.astype(np.int32), want[0].astype(np.float32), want[0].astype(np.float32), np.arange(n, dtype=np.int32),
+            np.ones(n, np.float32), np.ones(n, np.float32))
+    grad, _ = guarded(n, V, "f32")
+    if dtype == "f32":
+        got = _policy_run(view, "f32", 1.0, case, 0.0, 0.0, grad)["grad"]
+        ref = oracle.policy_loss(x, at, case[1].astype(np.float64), case[4])[3]
+        r = np.arange(n)
+        _near(got[r, at], ref[r, at], rel * np.abs(ref[r, at]) + 1e-15, "the token's gradient")
+    tokens, slp, kept = empty(n, torch.int32), empty(n), empty(n)
+    rp.sample_tokens(view, dev(np.full(n, 0.5)), tokens, slp, kept, workspace=workspace(view))
+    assert tokens.tolist() == at.tolist()
+    _near(slp.double().cpu(), want[0], rel * np.abs(want[0]) + 2e-16, "sampled")
+    rp.sample_tokens(view, dev(np.full(n, 0.5)), tokens, slp, kept, top_k=dev(np.full(n, 5), torch.int32), workspace=workspace(view))
+    assert tokens.tolist() == at.tolist()
+    _near(slp.double().cpu(), want[0], rel * np.abs(want[0]) + 2e-16, "sampled, top-k")
+
+
+@pytest.mark.parametrize("V", [40, 5000])
+def test_logits_near_the_end_of_fp32(V):
+    """Rows of +-3e38 (all alike, and beside ordinary ones) are sums like any other."""
+    import paper_2606_26997_amd as rp
+    say(f"huge logits {V}")
+    n = 4
+    view = torch.zeros(n, V, device="cuda")
+    view[0], view[1], view[2] = -3.0e38, 3.0e38, -3.0e38
+    view[2, 5] = 1.0
+    view[3] = -3.4028234663852886e38
+    x = view.double().cpu().numpy()
+    tokens = np.array([3, 3, 5, 3])
+    lp, H = empty(n), empty(n)
+    rp.token_logprobs(view, dev(tokens, torch.int32), lp, H, workspace=workspace(view))
+    want = oracle.token_logprobs(x, tokens)
+    _near(lp.double().cpu(), want[0], lse_bound(V) + U * np.abs(want[0]), "logprobs")
+    _near(H.double().cpu(), want[1], entropy_bound(V) + U * np.abs(want[1]), "entropy")
+    case = (tokens.astype(np.int32), want[0].astype(np.float32), want[0].astype(np.float32), np.zeros(n, np.int32),
+            np.ones(1, np.float32), np.ones(n, np.float32))
+    grad, _ = guarded(n, V, "f32")
+    _policy_check(x, view, "f32", 1.0, case, _policy_run(view, "f32", 1.0, case, 0.05, 0.01, grad), 0.05, 0.01)
+    got = rp_sample(view)
+    assert got[2] == 5 and all(0 <= t < V for t in got)
+
+
+def rp_sample(view):
+    import paper_2606_26997_amd as rp
+    tokens = empty(view.shape[0], torch.int32)
+    rp.sample_tokens(view, dev(np.full(view.shape[0], 0.4)), tokens, workspace=workspace(view))
+    return tokens.tolist()
