@@ -264,6 +264,7 @@ struct SampleArgs {
   int* tokens;
   float* logprobs;
   float* kept;
+  void* workspace;  // sample_workspace bytes
 };
 
 struct LogprobArgs {
@@ -327,6 +328,8 @@ hipError_t launch_prefill_kv_write(const PrefillArgs& a, int head_dim, bool fp8,
 hipError_t launch_prefill_attn(const PrefillArgs& a, int head_dim, int n_rep, hipStream_t stream);
 hipError_t launch_qk_prep(QkPrepArgs a, int head_dim, bool fp8, hipStream_t stream);
 hipError_t launch_grpo(const GrpoArgs& a, hipStream_t stream);
+// Bytes of workspace that sampling takes (0 for many shapes).
+size_t sample_workspace(int rows, int vocab, int dtype);
 hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_logprobs(const LogprobArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_policy(const PolicyArgs& a, int dtype, hipStream_t stream);

@@ -82,7 +82,7 @@ rp_status check_workspace(size_t need, const void* workspace, size_t bytes) {
   return RP_OK;
 }
 
-size_t workspace_need(const Rows&) { return 0; }
+size_t workspace_need(const Rows& r) { return rp::sample_workspace(r.args.rows, r.args.vocab, r.dtype); }
 
 }  // namespace
 
@@ -108,7 +108,7 @@ rp_status rp_sample_tokens(const rp_logits* logits, const rp_sampling* sampling,
   if (bad(u) || bad(tokens)) return fail(RP_ERR_INVALID_ARG, "u/tokens must be non-NULL and 4-byte aligned");
   if (bad_if_there(logprobs) || bad_if_there(kept_logprobs))
     return fail(RP_ERR_INVALID_ARG, "logprobs/kept_logprobs must be 4-byte aligned");
-  rp::SampleArgs a{r.args, nullptr, nullptr, nullptr, nullptr, u, tokens, logprobs, kept_logprobs};
+  rp::SampleArgs a{r.args, nullptr, nullptr, nullptr, nullptr, u, tokens, logprobs, kept_logprobs, workspace};
   if (sampling != nullptr) {
     a.temperature = sampling->temperature;
     a.top_k = sampling->top_k;
@@ -118,6 +118,8 @@ rp_status rp_sample_tokens(const rp_logits* logits, const rp_sampling* sampling,
       return fail(RP_ERR_INVALID_ARG, "temperature/top_k/top_p/min_p must be 4-byte aligned");
   }
   st = check_workspace(workspace_need(r), workspace, workspace_bytes);
+  if (st == RP_OK) st = rp::device_cus(&r.args.num_cus);
+  a.logits = r.args;
   return st == RP_OK ? done(rp::launch_sample(a, r.dtype, stream), "sampling") : st;
 }
 
@@ -130,8 +132,9 @@ rp_status rp_token_logprobs(const rp_logits* logits, const int32_t* tokens, doub
   if (st != RP_OK || r.args.rows == 0) return st;
   if (bad(tokens) || bad(logprobs) || bad_if_there(entropy))
     return fail(RP_ERR_INVALID_ARG, "tokens/logprobs must be non-NULL, and with entropy 4-byte aligned");
-  const rp::LogprobArgs a{r.args, tokens, 1.0 / temperature, logprobs, entropy};
   st = check_workspace(workspace_need(r), workspace, workspace_bytes);
+  if (st == RP_OK) st = rp::device_cus(&r.args.num_cus);
+  const rp::LogprobArgs a{r.args, tokens, 1.0 / temperature, logprobs, entropy};
   return st == RP_OK ? done(rp::launch_logprobs(a, r.dtype, stream), "log-probabilities") : st;
 }
 

@@ -27,6 +27,14 @@ typedef unsigned long long u64;
 constexpr int kBins = 1024;
 constexpr int kNoCrossing = 0x7FFFFFFF;
 
+// A listed token: its place in the order of keys, then of falling indices, and its weight.
+struct Token {
+  u64 place;
+  u64 mass;
+  __device__ inline uint32_t key() const { return (uint32_t)(place >> 32); }
+  __device__ inline uint32_t late() const { return (uint32_t)place; }  // ~index: more for lower indices
+};
+
 template <int NT>
 struct Lds {
   static constexpr int kWaves = NT / 64;
@@ -36,9 +44,12 @@ struct Lds {
   double d[kWaves];
   int i[kWaves];
   u64 q[kWaves];
+  static constexpr int kSmall = NT == 256 ? 128 : 256;  // lists that are sorted by counting
   u64 hist[kBins];
-  u64 mass[kList];
-  uint32_t key[kList], index[kList], work[kList];
+  Token list[kList];
+  uint32_t work[kList];
+  u64 over[kSmall];
+  int rank[kSmall];
   uint16_t top[kEntries * NT];
   u64 above;
   int bin, count, works, first, spare;
@@ -93,48 +104,225 @@ __device__ inline u64 mass_of(double w, double scale) {
 }
 
 // The row, and which vectors of it a thread has: wave w has the stretch of
-// `steps` * 64 vectors from w * steps * 64 on, in the order of indices.
+// `steps` * 64 vectors from w * steps * 64 on, in the order of indices; entry g of
+// a thread is the largest key of its vectors j with j >> shift == g.
 template <int DT, int NT>
 struct Row {
   static constexpr int E = Elem<DT>::kPerVec;
   const void* data;
-  int vocab, steps, shift;  // vectors j >> shift of a thread share an entry of lds.top
+  int vocab, steps, shift, entries;
   float max;
   double c;
+  __device__ inline Row(const LogitArgs& l, int n)
+      : data(static_cast<const char*>(l.data) + (long long)n * l.stride * Elem<DT>::kBytes),
+        vocab(l.vocab),
+        steps(cdiv(cdiv(l.vocab, E), NT)),
+        shift(0) {
+    while (cdiv(steps, 1 << shift) > Lds<NT>::kEntries) ++shift;
+    entries = cdiv(steps, 1 << shift);
+  }
   __device__ inline int vec(int thread, int j) const { return (thread / 64 * steps + j) * 64 + thread % 64; }
-  // f(vector, its logits) for this thread's vectors whose largest key is `upper` or more.
-  template <class F>
-  __device__ inline void each(const Lds<NT>& l, uint32_t upper, const F& f) const {
-    constexpr int U = 4;
-    for (int j0 = 0; j0 < steps; j0 += U) {
-      u32x4_any q[U];
-      bool has[U];
+  __device__ inline bool has(int thread, int j) const { return j < steps && vec(thread, j) * E < vocab; }
+  // f(vector, its logits) for this thread's vectors whose largest key is `upper` or more;
+  // U of them requested ahead (the code is U times there).
+  template <int U, class F>
+  __device__ __attribute__((always_inline)) inline void each(const Lds<NT>& l, uint32_t upper, const F& f) const {
+    const int tid = threadIdx.x;
+    u32x4_any next[U];
+    uint32_t wanted = 0;
+    const auto fetch = [&](int j0) __attribute__((always_inline)) {
+      wanted = 0;
 #pragma unroll
-      for (int k = 0; k < U; ++k) {
-        const int j = j0 + k, v = vec(threadIdx.x, j);
-        has[k] = j < steps && v * E < vocab && l.top[(j >> shift) * NT + threadIdx.x] >= upper;
-        if (has[k]) q[k] = load_vec<DT>(data, v, vocab);
+      for (int i = 0; i < U; ++i) {
+        const int j = j0 + i;
+        if (!has(tid, j) || l.top[(j >> shift) * NT + tid] < upper) continue;
+        next[i] = load_vec<DT>(data, vec(tid, j), vocab);
+        wanted |= 1u << i;
       }
+    };
+    fetch(0);
+#pragma unroll 1
+    for (int j0 = 0; j0 < steps; j0 += U) {
+      u32x4_any now[U];
 #pragma unroll
-      for (int k = 0; k < U; ++k) {
-        if (!has[k]) continue;
+      for (int i = 0; i < U; ++i) now[i] = next[i];
+      const uint32_t take = wanted;
+      fetch(j0 + U);
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (!(take >> i & 1)) continue;
         float x[E];
-        unpack<DT>(q[k], x);
-        f(vec(threadIdx.x, j0 + k), x);
+        unpack<DT>(now[i], x);
+        f(vec(tid, j0 + i), x);
       }
     }
   }
 };
 
-// The place, from the top of lds.hist, where the sums reach `need` (at most all
-// of it): its bin, and the sum above.
-template <int NT>
-__device__ inline int find_top(Lds<NT>& l, u64 need, u64& above) {
-  constexpr int PER = kBins / NT;
+// How row n is sampled. Greedy is top-1 at T = 1. c stays above 0, so that -inf
+// weighs nothing at T = inf too.
+struct How {
+  int k;        // vocab: all
+  double p, q;  // 1 and 0: all
+  double inv_t;
+  bool all, exact, light;  // exact: a border hangs on the row's whole sum; light: k few enough for a list
+  __device__ inline How(const SampleArgs& a, int n, int lightest) {
+    const int V = a.logits.vocab;
+    const float T = a.temperature != nullptr ? a.temperature[n] : 1.f;
+    const bool greedy = !(T > 0.f);
+    const int asked_k = greedy ? 1 : a.top_k != nullptr ? a.top_k[n] : 0;
+    const float asked_p = greedy || a.top_p == nullptr ? 1.f : a.top_p[n];
+    const float asked_q = greedy || a.min_p == nullptr ? 0.f : a.min_p[n];
+    k = asked_k > 0 && asked_k < V ? asked_k : V;
+    p = asked_p < 1.f ? fmax((double)asked_p, 0.0) : 1.0;
+    q = asked_q > 0.f ? fmin((double)asked_q, 1.0) : 0.0;
+    inv_t = greedy ? 1.0 : fmax(1.0 / (double)T, 1e-300);
+    light = k < V && k <= lightest;
+    all = k >= V && p >= 1.0 && q == 0.0;
+    exact = k >= V && (p < 1.0 || q == 0.0);
+  }
+};
+
+// What a pass over some of a stretch's vectors finds: the largest logit, and the
+// weights' sum relative to `ref`: in 64 bits (s), or in 32, the vector with the
+// largest logit (at) apart from the others.
+struct Scan {
+  float top = -INFINITY, ref = -INFINITY, group = 0.f, rest = 0.f;
+  double s = 0.0;
+  int at = -1;
+  bool bad = false;  // a NaN or +inf
+};
+
+// Entries first, first + stride, .. of the thread's vectors; put(entry, largest key).
+template <int DT, int NT, class Put>
+__device__ __attribute__((always_inline)) inline Scan scan(const Row<DT, NT>& r, int thread, int first, int stride,
+                                                           bool exact, const Put& put) {
+  constexpr int E = Elem<DT>::kPerVec, U = 4;
+  typedef Key<DT> K;
+  Scan o;
+  const float c32 = (float)fmin(r.c, 3e38);
+  const int each = (1 << r.shift) - 1, count = r.entries > first ? cdiv(r.entries - first, stride) << r.shift : 0;
+  const auto at = [&](int i) { return ((i >> r.shift) * stride + first) << r.shift | (i & each); };
+  u32x4_any next[U];
+  const auto fetch = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (i0 + i < count && r.has(thread, at(i0 + i))) next[i] = load_vec<DT>(r.data, r.vec(thread, at(i0 + i)), r.vocab);
+  };
+  uint32_t entry = 0;
+  fetch(0);
+#pragma unroll 1
+  for (int i0 = 0; i0 < count; i0 += U) {
+    u32x4_any now[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) now[i] = next[i];
+    fetch(i0 + U);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (i0 + i >= count) break;
+      const int j = at(i0 + i);
+      if (r.has(thread, j)) {
+        float x[E];
+        unpack<DT>(now[i], x);
+        float most = x[0];  // a NaN passes through
+#pragma unroll
+        for (int e = 1; e < E; ++e) most = __builtin_elementwise_maximum(most, x[e]);
+        o.bad = o.bad || !(most < INFINITY);
+        entry = max(entry, K::upper(K::of(most)));
+        if (!(most > -INFINITY)) {
+          // nothing to sum
+        } else if (exact) {
+          // The reference moves when a weight would pass 2^256, which 64 bits hold.
+          if (!((double)(most - o.ref) * r.c < 256.0)) {
+            o.s *= weight(o.ref, most, r.c);
+            o.ref = most;
+          }
+          double s = weight(x[0], o.ref, r.c);
+#pragma unroll
+          for (int e = 1; e < E; ++e) s += weight(x[e], o.ref, r.c);
+          o.s += s;
+        } else {
+          const bool more = most > o.top;
+          if (more) {
+            o.rest = (o.rest + o.group) * fast_exp2((o.top - most) * c32);
+            o.ref = most;
+            o.at = r.vec(thread, j);
+          }
+          float s = 0.f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) s += fast_exp2((x[e] - o.ref) * c32);
+          if (more) o.group = s;
+          else o.rest += s;
+        }
+        o.top = fmaxf(o.top, most);
+      }
+      if (((i0 + i) & each) == each) {
+        put(j >> r.shift, (uint16_t)entry);
+        entry = 0;
+      }
+    }
+  }
+  return o;
+}
+
+// A scan's sum relative to the maximum of the scans that it is joined with.
+template <int DT, int NT>
+__device__ inline double sum_to(const Scan& o, const Row<DT, NT>& r, float max, bool exact) {
+  if (!(o.ref > -INFINITY)) return 0.0;
+  if (exact) return o.s * weight(o.ref, max, r.c);
+  const float c32 = (float)fmin(r.c, 3e38);
+  if (o.top < max) return (double)((o.rest + o.group) * fast_exp2((o.ref - max) * c32));
+  // The vector with the maximum again, in 64 bits: where one token has nearly all
+  // the mass, ln Z is that of the rest.
+  float x[Elem<DT>::kPerVec];
+  unpack<DT>(load_vec<DT>(r.data, o.at, r.vocab), x);
+  double s = (double)o.rest;
+#pragma unroll
+  for (int e = 0; e < Elem<DT>::kPerVec; ++e) s += (double)fast_exp2((x[e] - max) * c32);
+  return s;
+}
+
+// Few rows leave most of the chip idle, so their stretches are scanned by workgroups
+// of their own (scan_kernel); their results, and the entries, go through memory.
+struct Part {
+  float top;
+  int bad;
+  double s;
+};
+constexpr int kSplit = 16, kSplitThreads = 1024, kScanThreads = 256;
+struct SplitRow {
+  Part part[kSplit];
+  uint16_t top[32 * kSplitThreads];
+};
+static_assert(kSplit * 64 == kSplitThreads && Lds<kSplitThreads>::kEntries == 32, "a stretch per wave");
+
+template <int DT>
+__global__ __launch_bounds__(kScanThreads) void scan_kernel(const SampleArgs a) {
+  __shared__ float lds_f[kScanThreads / 64];
+  __shared__ double lds_d[kScanThreads / 64];
+  const int n = blockIdx.x / kSplit, stretch = blockIdx.x % kSplit, tid = threadIdx.x;
+  SplitRow& out = static_cast<SplitRow*>(a.workspace)[n];
+  Row<DT, kSplitThreads> r(a.logits, n);
+  const How how(a, n, kSplitThreads / 2);
+  r.c = kLog2e64 * how.inv_t;
+  const int thread = stretch * 64 + tid % 64;
+  const Scan o = scan(r, thread, tid / 64, kScanThreads / 64, how.exact,
+                      [&](int g, uint16_t key) { out.top[g * kSplitThreads + thread] = key; });
+  const float top = block_max<kScanThreads>(o.top, lds_f);
+  const bool bad = __syncthreads_or(o.bad);
+  const double s = block_sum<kScanThreads>(bad ? 0.0 : sum_to(o, r, top, how.exact), lds_d);
+  if (tid == 0) out.part[stretch] = {top, bad ? 1 : 0, s};
+}
+
+// The place, from the top of BINS bins, where the sums of value(bin) reach `need`
+// (at most all of it): its bin, and the sum above.
+template <int NT, int BINS, class Value>
+__device__ inline int find_top(Lds<NT>& l, u64 need, u64& above, const Value& value) {
+  constexpr int PER = BINS / NT;
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   u64 h[PER], sum = 0;
 #pragma unroll
-  for (int k = 0; k < PER; ++k) sum += h[k] = l.hist[kBins - 1 - (tid * PER + k)];
+  for (int k = 0; k < PER; ++k) sum += h[k] = value(BINS - 1 - (tid * PER + k));
   u64 upto = sum;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -159,7 +347,7 @@ __device__ inline int find_top(Lds<NT>& l, u64 need, u64& above) {
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       if (run < need && need <= run + h[k]) {
-        l.bin = kBins - 1 - (tid * PER + k);
+        l.bin = BINS - 1 - (tid * PER + k);
         l.above = run;
       }
       run += h[k];
@@ -168,6 +356,11 @@ __device__ inline int find_top(Lds<NT>& l, u64 need, u64& above) {
   __syncthreads();
   above = l.above;
   return l.bin;
+}
+
+template <int NT>
+__device__ inline int find_top(Lds<NT>& l, u64 need, u64& above) {
+  return find_top<NT, kBins>(l, need, above, [&](int bin) { return l.hist[bin]; });
 }
 
 template <int NT>
@@ -183,7 +376,7 @@ struct Cut {
   u64 above;
 };
 template <int NT, class Items>
-__device__ inline Cut descend(Lds<NT>& l, uint32_t lo, uint32_t hi, u64 need, const Items& items) {
+__device__ __attribute__((always_inline)) inline Cut descend(Lds<NT>& l, uint32_t lo, uint32_t hi, u64 need, const Items& items) {
   u64 over = 0;
   uint32_t width = hi - lo;
   while (true) {
@@ -205,11 +398,12 @@ __device__ inline Cut descend(Lds<NT>& l, uint32_t lo, uint32_t hi, u64 need, co
   }
 }
 
-// Lists the tokens that `keep` takes, from vectors whose largest key is `upper` or more; whether they fit.
-template <int DT, int NT, class Keep>
-__device__ inline bool gather(Lds<NT>& l, const Row<DT, NT>& r, uint32_t upper, double scale, const Keep& keep) {
+// Lists the tokens whose key is tau or more; whether they fit.
+template <int DT, int NT>
+__device__ inline bool gather(Lds<NT>& l, const Row<DT, NT>& r, uint32_t tau, double scale) {
   constexpr int E = Elem<DT>::kPerVec;
   const int tid = threadIdx.x, entries = cdiv(r.steps, 1 << r.shift);
+  const uint32_t upper = Key<DT>::upper(tau);
   __syncthreads();
   if (tid == 0) l.count = l.works = 0;
   __syncthreads();
@@ -230,115 +424,59 @@ __device__ inline bool gather(Lds<NT>& l, const Row<DT, NT>& r, uint32_t upper, 
 #pragma unroll
     for (int k = 0; k < E; ++k) {
       const uint32_t key = Key<DT>::of(x[k]);
-      if (!keep(x[k], key)) continue;
+      if (key < tau) continue;
       const int at = atomicAdd(&l.count, 1);
       if (at >= Lds<NT>::kList) continue;
-      l.key[at] = key;
-      l.index[at] = v * E + k;
-      l.mass[at] = mass_of(weight(x[k], r.max, r.c), scale);
+      l.list[at] = {(u64)key << 32 | ~(uint32_t)(v * E + k), mass_of(weight(x[k], r.max, r.c), scale)};
     }
   }
   __syncthreads();
   return l.count <= Lds<NT>::kList;
 }
 
-template <int DT, int NT>
+// SPLIT: scan_kernel has been over the row.
+template <int DT, int NT, bool SPLIT>
 __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   __shared__ Lds<NT> l;
   typedef Key<DT> K;
   constexpr int E = Elem<DT>::kPerVec, kWaves = Lds<NT>::kWaves;
   const int n = blockIdx.x, V = a.logits.vocab, tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
-  Row<DT, NT> r;
-  r.data = static_cast<const char*>(a.logits.data) + (long long)n * a.logits.stride * Elem<DT>::kBytes;
-  r.vocab = V;
-  r.steps = cdiv(cdiv(V, E), NT);
-  r.shift = 0;
-  while (cdiv(r.steps, 1 << r.shift) > Lds<NT>::kEntries) ++r.shift;
+  Row<DT, NT> r(a.logits, n);
+  const How how(a, n, NT / 2);
+  r.c = kLog2e64 * how.inv_t;
+  const int k = how.k;
+  const double p = how.p, q = how.q, inv_t = how.inv_t;
+  const bool light_k = how.light, all = how.all;
 
-  // Greedy is top-1 at T = 1. c stays above 0, so that -inf weighs nothing at T = inf too.
-  float T = a.temperature != nullptr ? a.temperature[n] : 1.f;
-  const bool greedy = !(T > 0.f);
-  const int asked_k = greedy ? 1 : a.top_k != nullptr ? a.top_k[n] : 0;
-  const int k = asked_k > 0 && asked_k < V ? asked_k : V;
-  const float asked_p = greedy || a.top_p == nullptr ? 1.f : a.top_p[n];
-  const double p = asked_p < 1.f ? fmax((double)asked_p, 0.0) : 1.0;
-  const float asked_q = greedy || a.min_p == nullptr ? 0.f : a.min_p[n];
-  const double q = asked_q > 0.f ? fmin((double)asked_q, 1.0) : 0.0;
-  const double inv_t = greedy ? 1.0 : fmax(1.0 / (double)T, 1e-300);
-  r.c = kLog2e64 * inv_t;
-  const float c32 = (float)fmin(r.c, 3e38);
-  const bool light_k = k < V && k <= NT / 2;
-  const bool all = k >= V && p >= 1.0 && q == 0.0;
-  const bool exact = k >= V && (p < 1.0 || q == 0.0);
-
-  // ---- the row's maximum, its sum and the vectors' largest keys
-  // In 32 bits: sums of the vector with the thread's largest logit, and of the others.
-  float top = -INFINITY, ref = -INFINITY, group = 0.f, rest = 0.f;
-  double s64 = 0.0;
-  int at_top = -1;
+  float top = -INFINITY;  // the thread's largest logit (SPLIT: or less than that, by the bits that the entries lack)
   bool bad = false;
-  for (int g = 0; g < Lds<NT>::kEntries; ++g) l.top[g * NT + tid] = 0;
-  {
-    constexpr int U = 4;
-    u32x4_any next[U];
-    const auto fetch = [&](int j0) {
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int v = r.vec(tid, j0 + i);
-        if (j0 + i < r.steps && v * E < V) next[i] = load_vec<DT>(r.data, v, V);
-      }
-    };
-    fetch(0);
-    for (int j0 = 0; j0 < r.steps; j0 += U) {
-      u32x4_any now[U];
-#pragma unroll
-      for (int i = 0; i < U; ++i) now[i] = next[i];
-      fetch(j0 + U);
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int j = j0 + i;
-        if (j >= r.steps || r.vec(tid, j) * E >= V) continue;
-        float x[E];
-        unpack<DT>(now[i], x);
-        float most = x[0];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          most = fmaxf(most, x[e]);
-          bad = bad || !(x[e] < INFINITY);
-        }
-        if (!(most > -INFINITY)) continue;
-        const uint16_t entry = (uint16_t)K::upper(K::of(most));
-        uint16_t& slot = l.top[(j >> r.shift) * NT + tid];
-        slot = max(slot, entry);
-        if (exact) {
-          // The reference moves when a weight would pass 2^256, which 64 bits hold.
-          if (!((double)(most - ref) * r.c < 256.0)) {
-            s64 *= weight(ref, most, r.c);
-            ref = most;
-          }
-          double s = 0.0;
-#pragma unroll
-          for (int e = 0; e < E; ++e) s += weight(x[e], ref, r.c);
-          s64 += s;
-        } else {
-          const bool more = most > top;
-          if (more) {
-            rest = (rest + group) * fast_exp2((top - most) * c32);
-            ref = most;
-            at_top = r.vec(tid, j);
-          }
-          float s = 0.f;
-#pragma unroll
-          for (int e = 0; e < E; ++e) s += fast_exp2((x[e] - ref) * c32);
-          if (more) group = s;
-          else rest += s;
-        }
-        top = fmaxf(top, most);
-      }
+  if constexpr (SPLIT) {
+    const SplitRow& in = static_cast<const SplitRow*>(a.workspace)[n];
+    const Part part = in.part[tid % kSplit];
+    r.max = wave_max(part.top);
+    bad = __ballot(part.bad != 0) != 0;
+    if (tid < kSplit && part.top > -INFINITY)
+      l.d[tid] = part.s * (how.exact ? weight(part.top, r.max, r.c)
+                                     : (double)fast_exp2((part.top - r.max) * (float)fmin(r.c, 3e38)));
+    else if (tid < kSplit) l.d[tid] = 0.0;
+    uint32_t most = 0;
+    for (int g = 0; g < r.entries; ++g) {
+      const uint16_t key = in.top[g * NT + tid];
+      l.top[g * NT + tid] = key;
+      most = max(most, (uint32_t)key);
+    }
+    const uint32_t o = most << 16;
+    if (most > 0x007Fu) top = __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+  } else {
+    const Scan o = scan(r, tid, 0, 1, how.exact, [&](int g, uint16_t key) { l.top[g * NT + tid] = key; });
+    top = o.top;
+    r.max = block_max<NT>(top, l.f);
+    bad = __syncthreads_or(o.bad);
+    if (!bad && r.max > -INFINITY) {
+      const double s = wave_sum(sum_to(o, r, r.max, how.exact));
+      if (lane == 0) l.d[wave] = s;
     }
   }
-  r.max = block_max<NT>(top, l.f);
-  bad = __syncthreads_or(bad);
   if (bad || r.max == -INFINITY) {
     if (tid == 0) {
       const float none = bad ? NAN : -INFINITY;
@@ -348,24 +486,6 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     }
     return;
   }
-  if (exact) {
-    if (ref > -INFINITY) s64 *= weight(ref, r.max, r.c);
-  } else {
-    // The vector with the row's maximum again, in 64 bits: where one token has nearly
-    // all the mass, ln Z is that of the rest.
-    if (top == r.max) {
-      float x[E];
-      unpack<DT>(load_vec<DT>(r.data, at_top, V), x);
-      s64 = (double)rest;
-#pragma unroll
-      for (int e = 0; e < E; ++e) s64 += (double)fast_exp2((x[e] - top) * c32);
-    } else if (ref > -INFINITY) {
-      s64 = (double)((rest + group) * fast_exp2((ref - r.max) * c32));
-    }
-  }
-  const double wave_part = wave_sum(s64);
-  __syncthreads();
-  if (lane == 0) l.d[wave] = wave_part;
   __syncthreads();
   double Z = 0.0;
 #pragma unroll
@@ -378,7 +498,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   if (!(u >= 0.f)) u = 0.f;
   const double part = (double)fminf(u, 0x1.fffffep-1f);
 
-  const auto finish = [&](int token, double total) {
+  const auto finish = [&](int token, double total) __attribute__((always_inline)) {
     const double z = ((double)Elem<DT>::get(r.data, max(token, 0)) - (double)r.max) * inv_t;
     a.tokens[n] = token;
     if (a.logprobs != nullptr) a.logprobs[n] = (float)(z - log(Z));
@@ -387,46 +507,115 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
 
   uint32_t cut = K::kNegInf;  // keys above it are kept, and the first `ties` at it
   int ties = 0;
-  bool listed = false;
+  bool listed = false, summed = all;  // summed: l.d and l.i hold the stretches' kept weight and ties
+  if (all && lane == 0) l.i[wave] = 0;
   if (!all) {
-    // A key that `want` threads' largest ones, and so as many tokens, reach.
+    // A key down to which the threads' largest logits alone are `need` tokens (or, by
+    // mass, weigh that much), so that all that is kept lies there; 0 if they never do.
     const float least_top = -block_max<NT>(top > -INFINITY ? -top : -INFINITY, l.f);
-    const auto reached = [&](int want) {
+    const auto reached = [&](bool by_mass, u64 need) __attribute__((always_inline)) {
       const float fit = fmaxf(fminf(r.max - least_top, 1e30f), 1e-30f);
       const int bin = kBins - 1 - (int)fminf((r.max - top) * ((kBins - 2) / fit), kBins - 1.f);
       const bool has = top > -INFINITY;
+      const u64 mine = !has ? 0 : by_mass ? mass_of(weight(top, r.max, r.c), scale) : 1;
       __syncthreads();
       clear<NT>(l.hist);
       if (tid == 0) l.least = 0xFFFFFFFFu;
       __syncthreads();
-      if (has) atomicAdd(&l.hist[bin], 1ull);
-      const int threads = __syncthreads_count(has);
-      if (threads < want) return K::kNegInf + 1;
+      if (has) atomicAdd(&l.hist[bin], mine);
+      if (block_sum<NT>(mine, l.q) < need) return 0u;
       u64 above;
-      const int at = find_top(l, (u64)want, above);
+      const int at = find_top(l, need, above);
       if (has && bin >= at) atomicMin(&l.least, K::of(top));
       __syncthreads();
       return l.least;
     };
-    const auto from_list = [&](auto&& f) {
+    const auto from_list = [&](auto&& f) __attribute__((always_inline)) {
       const int count = l.count;
-      for (int i = tid; i < count; i += NT) f(l.key[i], l.index[i], l.mass[i]);
+      for (int i = tid; i < count; i += NT) f(l.list[i].key(), l.list[i].late(), l.list[i].mass);
     };
     const uint32_t most = K::of(r.max);
     const bool probe = k >= V && p < 1.0;
-    if (light_k || probe) {
-      const uint32_t tau = reached(light_k ? k : NT / 2);
-      listed = gather<DT, NT>(l, r, K::upper(tau), scale, [&](float, uint32_t key) { return key >= tau; });
+    const u64 need_p = (u64)fmax(ceil(p * Z * scale), 1.0);  // where every token counts
+    uint32_t key_q = 0;  // the least key of weight q or more
+    if (q > 0.0) {
+      const double least = (double)r.max + log2(q) / r.c;
+      key_q = K::of((float)least);
+      if (!((double)K::logit(key_q) >= least)) ++key_q;
+      key_q = min(max(key_q, K::kNegInf + 1), most);
+    }
+    uint32_t tau = 0;
+    if (light_k) tau = max(reached(false, (u64)k), K::kNegInf + 1);
+    else if (probe) tau = reached(true, need_p);
+    else if (k >= V) tau = key_q;
+    if (tau != 0)
+      listed = gather(l, r, tau, scale);
+
+    // A short list: every token counts those before it, in the order of keys and in
+    // that of indices, the waves sharing out whom they count.
+    if (listed && l.count <= Lds<NT>::kSmall) {
+      const int count = l.count, blocks = cdiv(count, 64), shares = kWaves / blocks;
+      const int at = wave % blocks * 64 + lane, share = wave / blocks;
+      const int from = share * count / shares, to = share < shares ? (share + 1) * count / shares : from;
+      const bool is = tid < count;
+      const auto tally = [&](auto&& add) __attribute__((always_inline)) {
+        if (at < count) add(l.list[at].place);
+      };
+      if (is) {
+        l.rank[tid] = 0;
+        l.over[tid] = 0;
+      }
+      __syncthreads();
+      tally([&](u64 place) {
+        int rank = 0;
+        u64 over = 0;
+        for (int j = from; j < to; ++j) {
+          const Token t = l.list[j];
+          rank += t.place > place ? 1 : 0;
+          over += t.place > place ? t.mass : 0;
+        }
+        if (from < to) {
+          atomicAdd(&l.rank[at], rank);
+          atomicAdd(&l.over[at], over);
+        }
+      });
+      __syncthreads();
+      const Token mine = is ? l.list[tid] : Token{0, 0};
+      bool in = is && l.rank[tid] < k;
+      if (p < 1.0) {
+        u64 need = need_p;
+        if (k < V) need = (u64)fmax(ceil(p * (double)block_sum<NT>(in ? mine.mass : 0, l.q)), 1.0);
+        in = in && l.over[tid] < need;
+      }
+      in = in && mine.key() >= key_q;
+      const u64 mass = in ? mine.mass : 0, sum = block_sum<NT>(mass, l.q);
+      const u64 need = min((u64)floor(part * (double)sum) + 1, sum);
+      if (is) {
+        l.list[tid].mass = mass;
+        l.over[tid] = 0;
+      }
+      __syncthreads();
+      tally([&](u64 place) {
+        u64 upto = 0;
+        for (int j = from; j < to; ++j) {
+          const Token t = l.list[j];
+          upto += t.late() >= (uint32_t)place ? t.mass : 0;
+        }
+        if (from < to) atomicAdd(&l.over[at], upto);
+      });
+      __syncthreads();
+      if (mass > 0 && l.over[tid] >= need && l.over[tid] - mass < need) finish((int)~mine.late(), (double)sum / scale);
+      return;
     }
     const int listed_n = l.count;
 
     // The key at which the tokens' masses (their number, where `count`) reach
     // `need`, from the row itself: by equal steps of the logits down to `low`,
     // then within one of those.
-    const auto from_row = [&](bool count, u64 need, float low, uint32_t upper) {
+    const auto from_row = [&](bool count, u64 need, float low, uint32_t upper) __attribute__((always_inline)) {
       const float fit = fmaxf(fminf(r.max - low, 1e30f), 1e-30f), per = (kBins - 2) / fit;
-      const auto step = [&](float x) { return kBins - 1 - (int)fminf((r.max - x) * per, kBins - 1.f); };
-      const auto one = [&](float x) { return count ? 1ull : mass_of(weight(x, r.max, r.c), scale); };
+      const auto step = [&](float x) __attribute__((always_inline)) { return kBins - 1 - (int)fminf((r.max - x) * per, kBins - 1.f); };
+      const auto one = [&](float x) __attribute__((always_inline)) { return count ? 1ull : mass_of(weight(x, r.max, r.c), scale); };
       __syncthreads();
       clear<NT>(l.hist);
       if (tid == 0) {
@@ -434,7 +623,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
         l.most = 0;
       }
       __syncthreads();
-      r.each(l, upper, [&](int, const float (&x)[E]) {
+      r.template each<1>(l, upper, [&](int, const float (&x)[E]) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
           if (x[e] > -INFINITY) atomicAdd(&l.hist[step(x[e])], one(x[e]));
@@ -443,60 +632,155 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       u64 above;
       const int at = find_top(l, need, above);
       need -= above < need ? above : need;
-      // Every key of that step, and a threshold for the vectors that hold them.
+      // The keys of that step, and a threshold for the vectors that hold them.
       const float edge = at == 0 ? -INFINITY : r.max - (float)(kBins - at) / per;
       const float slack = at == 0 ? 0.f : fabsf(edge) * 1e-5f + fit * 1e-4f;
       const uint32_t edge_upper = max(upper, at == 0 ? 0u : K::upper(K::of(edge - slack)));
-      const bool fits = gather<DT, NT>(l, r, edge_upper, scale, [&](float x, uint32_t key) {
-        const bool in = x > -INFINITY && step(x) == at;
-        if (in) {
-          atomicMin(&l.least, key);
-          atomicMax(&l.most, key);
-        }
-        return in;
+      uint32_t lo = 0xFFFFFFFFu, hi = 0;
+      r.template each<1>(l, edge_upper, [&](int, const float (&x)[E]) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (x[e] > -INFINITY && step(x[e]) == at) {
+            lo = min(lo, K::of(x[e]));
+            hi = max(hi, K::of(x[e]));
+          }
       });
-      Cut found;
-      if (fits) {
-        found = descend(l, l.least, l.most, need, [&](auto&& f) {
-          from_list([&](uint32_t key, uint32_t, u64 mass) { f(key, count ? 1ull : mass); });
-        });
-      } else {
-        __syncthreads();
-        if (tid == 0) {
-          l.least = 0xFFFFFFFFu;
-          l.most = 0;
-        }
-        __syncthreads();
-        uint32_t lo = 0xFFFFFFFFu, hi = 0;
-        r.each(l, edge_upper, [&](int, const float (&x)[E]) {
+      atomicMin(&l.least, lo);
+      atomicMax(&l.most, hi);
+      __syncthreads();
+      lo = l.least;
+      hi = l.most;
+      Cut found = descend(l, lo, hi, need, [&](auto&& f) {
+        r.template each<1>(l, edge_upper, [&](int, const float (&x)[E]) {
 #pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (x[e] > -INFINITY && step(x[e]) == at) {
-              lo = min(lo, K::of(x[e]));
-              hi = max(hi, K::of(x[e]));
-            }
+          for (int e = 0; e < E; ++e) {
+            const uint32_t key = K::of(x[e]);
+            if (key >= lo && key <= hi) f(key, one(x[e]));
+          }
         });
-        atomicMin(&l.least, lo);
-        atomicMax(&l.most, hi);
-        __syncthreads();
-        lo = l.least;
-        hi = l.most;
-        found = descend(l, lo, hi, need, [&](auto&& f) {
-          r.each(l, edge_upper, [&](int, const float (&x)[E]) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const uint32_t key = K::of(x[e]);
-              if (key >= lo && key <= hi) f(key, one(x[e]));
-            }
-          });
-        });
-      }
+      });
       found.above += above;
       return found;
     };
 
+    const auto tokens_at_all = [&] __attribute__((always_inline)) {
+      int finite = 0;
+      r.template each<1>(l, 0, [&](int, const float (&x)[E]) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) finite += x[e] > -INFINITY ? 1 : 0;
+      });
+      return block_sum<NT>(finite, l.i);
+    };
+    // Where the tokens that are kept are many: their number by equal steps of the
+    // logits says which steps the cut lies in (their weights, approximately); then
+    // one pass sums what is above those steps, by stretch, and lists what is in them.
+    // Tokens at `least` and below do not count: LDS would add to one bin for most of
+    // a wave. False where that does not settle it.
+    const auto wide = [&](bool by_mass, u64 need, float low, uint32_t upper, float least) __attribute__((always_inline)) {
+      constexpr int BINS = 2 * kBins;
+      uint32_t* counts = reinterpret_cast<uint32_t*>(l.hist);
+      const float fit = fmaxf(fminf(r.max - low, 1e30f), 1e-30f), per = (BINS - 2) / fit;
+      const auto step = [&](float x) __attribute__((always_inline)) { return BINS - 1 - (int)fminf((r.max - x) * per, BINS - 1.f); };
+      __syncthreads();
+      clear<NT>(l.hist);
+      __syncthreads();
+      r.template each<4>(l, upper, [&](int, const float (&x)[E]) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (x[e] > least) atomicAdd(&counts[step(x[e])], 1u);
+      });
+      __syncthreads();
+      const auto value = [&](int bin) __attribute__((always_inline)) {
+        const u64 n = counts[bin];
+        return by_mass && n > 0 ? n * mass_of(weight(r.max - (BINS - 0.5f - bin) / per, r.max, r.c), scale) : n;
+      };
+      u64 above;
+      const u64 slack = by_mass ? need >> 10 : 0;
+      const int hi = find_top<NT, BINS>(l, need - slack, above, value) + (by_mass ? 1 : 0);
+      const u64 above_count = above;  // where it is the number of tokens
+      __syncthreads();
+      const int lo = by_mass ? find_top<NT, BINS>(l, need + slack, above, value) - 1 : hi;
+      if (lo <= 0 || (key_q > 0 && step(K::logit(key_q)) > hi)) return false;
+      const float edge = r.max - (float)(BINS - lo) / per;
+      const uint32_t edge_upper = max(upper, K::upper(K::of(edge - (fabsf(edge) * 1e-5f + fit * 1e-4f))));
+      __syncthreads();
+      if (tid == 0) {
+        l.count = 0;
+        l.least = 0xFFFFFFFFu;
+        l.most = 0;
+      }
+      __syncthreads();
+      double s = 0.0;
+      r.template each<4>(l, edge_upper, [&](int v, const float (&x)[E]) {
+        uint32_t in = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int at = x[e] > -INFINITY ? step(x[e]) : 0;
+          if (at > hi) s += weight(x[e], r.max, r.c);
+          else if (at >= lo) in |= 1u << e;
+        }
+        for (; in != 0; in &= in - 1) {
+          const int i = v * E + __builtin_ctz(in), place = atomicAdd(&l.count, 1);
+          const float y = Elem<DT>::get(r.data, i);
+          const uint32_t key = K::of(y);
+          atomicMin(&l.least, key);
+          atomicMax(&l.most, key);
+          if (place < Lds<NT>::kList)
+            l.list[place] = {(u64)key << 32 | ~(uint32_t)i, mass_of(weight(y, r.max, r.c), scale)};
+        }
+      });
+      s = wave_sum(s);
+      if (lane == 0) l.d[wave] = s;
+      __syncthreads();
+      if (l.count > Lds<NT>::kList || l.count == 0) return false;
+      double over = 0.0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) over += l.d[w];
+      u64 sum = 0;
+      from_list([&](uint32_t, uint32_t, u64 mass) { sum += by_mass ? mass : 1; });
+      sum = block_sum<NT>(sum, l.q);
+      const u64 so_far = by_mass ? (u64)(over * scale) : above_count;
+      if (so_far >= need || so_far + sum < need) return false;
+      const Cut found = descend(l, l.least, l.most, need - so_far, [&](auto&& f) {
+        from_list([&](uint32_t key, uint32_t, u64 mass) { f(key, by_mass ? mass : 1ull); });
+      });
+      const u64 rest = need - so_far - found.above;
+      const u64 each = by_mass ? mass_of(weight(K::logit(found.key), r.max, r.c), scale) : 1;
+      cut = found.key;
+      ties = (int)min(each > 0 ? (rest + each - 1) / each : (u64)V, (u64)V);
+      if (key_q > cut) {
+        cut = key_q;
+        ties = V;
+      }
+      // What the list adds to each stretch.
+      __syncthreads();
+      if (tid < kWaves) {
+        l.q[tid] = 0;
+        l.i[tid] = 0;
+      }
+      __syncthreads();
+      from_list([&](uint32_t key, uint32_t late, u64 mass) {
+        const int w = (int)(~late) / (r.steps * 64 * E);
+        if (key > cut) atomicAdd(&l.q[w], mass);
+        if (key == cut) atomicAdd(&l.i[w], 1);
+      });
+      __syncthreads();
+      if (tid < kWaves) l.d[tid] += (double)l.q[tid] / scale;
+      __syncthreads();
+      return true;
+    };
+    if (!listed && probe) {
+      // Tokens of less than (1 - p) Z / V each sum to less than (1 - p) Z: none of them is in the nucleus.
+      const float low = fmaxf((float)((double)r.max + log2((1.0 - p) * Z / V) / r.c), -3e38f);
+      const float slack = fabsf(low) * 1e-5f + (r.max - low) * 1e-5f;
+      const bool sure = low > -3e38f;
+      summed = wide(true, need_p, low, sure ? K::upper(K::of(low - slack)) : 0, sure ? low - slack : -INFINITY);
+    } else if (!listed && k < V && p >= 1.0 && tokens_at_all() > k) {
+      summed = wide(false, (u64)k, r.max - 2.f * (r.max - least_top), 0, -INFINITY);
+    }
+
     u64 kept_mass = 0;  // of the top-k tokens
-    if (k < V) {
+    if (k < V && !summed) {
       Cut found = {K::kNegInf, 0};
       bool whole = false;
       if (listed) {
@@ -506,12 +790,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
             from_list([&](uint32_t key, uint32_t, u64) { f(key, 1ull); });
           });
       } else {
-        int finite = 0;
-        r.each(l, 0, [&](int, const float (&x)[E]) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) finite += x[e] > -INFINITY ? 1 : 0;
-        });
-        whole = block_sum<NT>(finite, l.i) <= k;
+        whole = tokens_at_all() <= k;
         if (!whole) found = from_row(true, (u64)k, r.max - 2.f * (r.max - least_top), 0);
       }
       if (!whole) {
@@ -523,7 +802,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
         if (listed) {
           from_list([&](uint32_t key, uint32_t, u64 mass) { sum += key > cut ? mass : 0; });
         } else {
-          r.each(l, K::upper(cut), [&](int, const float (&x)[E]) {
+          r.template each<1>(l, K::upper(cut), [&](int, const float (&x)[E]) {
 #pragma unroll
             for (int e = 0; e < E; ++e)
               if (K::of(x[e]) > cut) sum += mass_of(weight(x[e], r.max, r.c), scale);
@@ -533,17 +812,10 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
         if (ties > 0) kept_mass += (u64)ties * mass_of(weight(K::logit(cut), r.max, r.c), scale);
       }
     }
-    if (p < 1.0) {
-      const double want = p * (k < V ? (double)kept_mass : Z * scale);
-      const u64 need = (u64)fmax(ceil(want), 1.0);
-      bool enough = listed;
-      if (probe && listed) {
-        u64 sum = 0;
-        from_list([&](uint32_t, uint32_t, u64 mass) { sum += mass; });
-        enough = block_sum<NT>(sum, l.q) >= need;
-      }
+    if (p < 1.0 && !summed) {
+      const u64 need = k < V ? (u64)fmax(ceil(p * (double)kept_mass), 1.0) : need_p;
       Cut found;
-      if (enough) {
+      if (listed) {
         found = descend(l, K::kNegInf + 1, most, need, [&](auto&& f) {
           from_list([&](uint32_t key, uint32_t, u64 mass) { f(key, mass); });
         });
@@ -563,24 +835,14 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
         cut = found.key;
       }
     }
-    if (q > 0.0) {
-      // The least logit of weight q or more.
-      const double least = (double)r.max + log2(q) / r.c;
-      float x = (float)least;
-      uint32_t key = K::of(x);
-      if (!((double)K::logit(key) >= least)) ++key;
-      key = min(key, most);
-      if (key > cut) {
-        cut = key;
-        ties = V;
-      }
+    if (key_q > cut && !summed) {
+      cut = key_q;
+      ties = V;
     }
 
     // ---- the token, where all that may be kept fits into a list
-    if (!listed)
-      listed = gather<DT, NT>(l, r, K::upper(cut), scale, [&](float x, uint32_t key) {
-        return key >= cut && x > -INFINITY;
-      });
+    if (!listed && !summed)
+      listed = gather(l, r, max(cut, K::kNegInf + 1), scale);
     if (listed) {
       int equal = 0;
       from_list([&](uint32_t key, uint32_t, u64) { equal += key == cut ? 1 : 0; });
@@ -589,13 +851,13 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       uint32_t last_tie = 0;
       if (ties > 0 && ties < equal)
         last_tie = descend(l, ~(uint32_t)(V - 1), ~0u, (u64)ties, [&](auto&& f) {
-          from_list([&](uint32_t key, uint32_t index, u64) {
-            if (key == cut) f(~index, 1ull);
+          from_list([&](uint32_t key, uint32_t late, u64) {
+            if (key == cut) f(late, 1ull);
           });
         }).key;
-      const auto kept = [&](auto&& f) {
-        from_list([&](uint32_t key, uint32_t index, u64 mass) {
-          if (key > cut || (key == cut && ties > 0 && ~index >= last_tie)) f(~index, mass);
+      const auto kept = [&](auto&& f) __attribute__((always_inline)) {
+        from_list([&](uint32_t key, uint32_t late, u64 mass) {
+          if (key > cut || (key == cut && ties > 0 && late >= last_tie)) f(late, mass);
         });
       };
       u64 sum = 0;
@@ -612,16 +874,16 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   // the stretch that the border lies in.
   const uint32_t upper = K::upper(cut);
   const double w_cut = ties > 0 ? weight(K::logit(cut), r.max, r.c) : 0.0;
-  const auto held = [&](double mass, int count) { return mass + w_cut * (double)min(count, ties); };
-  const auto add = [&](float x, double& s, int& t) {
+  const auto held = [&](double mass, int count) __attribute__((always_inline)) { return mass + w_cut * (double)min(count, ties); };
+  const auto add = [&](float x, double& s, int& t) __attribute__((always_inline)) {
     const uint32_t key = K::of(x);
     if (key > cut) s += weight(x, r.max, r.c);
     if (key == cut) ++t;
   };
-  if (!all) {
+  if (!summed) {
     double s = 0.0;
     int t = 0;
-    r.each(l, upper, [&](int, const float (&x)[E]) {
+    r.template each<1>(l, upper, [&](int, const float (&x)[E]) {
 #pragma unroll
       for (int e = 0; e < E; ++e) add(x[e], s, t);
     });
@@ -632,36 +894,42 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       l.d[wave] = s;
       l.i[wave] = t;
     }
-    __syncthreads();
-  } else if (lane == 0) {
-    l.i[wave] = 0;
   }
   __syncthreads();
-  double before = 0.0, total_mass = 0.0;
-  int tie_before = 0, total_ties = 0;
+  // Every wave finds the stretch, its lanes w < kWaves holding the sums up to stretch w.
+  double upto_w = lane < kWaves ? l.d[lane] : 0.0;
+  int ties_w = lane < kWaves ? l.i[lane] : 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    total_mass += l.d[w];
-    total_ties += l.i[w];
+  for (int o = 1; o < kWaves; o <<= 1) {
+    const double us = __shfl_up(upto_w, o);
+    const int ut = __shfl_up(ties_w, o);
+    if (lane >= o) {
+      upto_w += us;
+      ties_w += ut;
+    }
   }
-  const double total = held(total_mass, total_ties), target = part * total;
-  int where = 0;
-  for (; where < kWaves - 1 && !(held(before + l.d[where], tie_before + l.i[where]) > target); ++where) {
-    before += l.d[where];
-    tie_before += l.i[where];
-  }
+  const double total = held(__shfl(upto_w, kWaves - 1), __shfl(ties_w, kWaves - 1)), target = part * total;
+  const u64 crossed = __ballot(lane < kWaves && held(upto_w, ties_w) > target) | 1ull << (kWaves - 1);
+  const int where = __builtin_ctzll(crossed);
+  double before = where > 0 ? __shfl(upto_w, max(where - 1, 0)) : 0.0;
+  int tie_before = where > 0 ? __shfl(ties_w, max(where - 1, 0)) : 0;
   // Sums in another order may miss the crossing by a rounding; then it is the stretch's last kept token.
   const int base = where * r.steps * 64, vectors = r.steps * 64;
   int spare_v = -1, spare_t = 0;
   double spare_s = 0.0;
-  const auto walk = [&](int v, double ms, int mt, double limit) {
+  // The first token of a vector that passes the limit, or its last kept one.
+  const auto walk = [&](int v, double ms, int mt, double limit) __attribute__((always_inline)) {
+    float x[E];
+    unpack<DT>(load_vec<DT>(r.data, v, V), x);
     int found = -1, last = -1;
     double at = held(ms, mt);
-    for (int e = 0; e < E && v * E + e < V; ++e) {
-      add(Elem<DT>::get(r.data, v * E + e), ms, mt);
-      if (held(ms, mt) > limit && found < 0) found = v * E + e;
-      if (held(ms, mt) > at) last = v * E + e;
-      at = held(ms, mt);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      add(x[e], ms, mt);
+      const double now = held(ms, mt);
+      if (now > limit && found < 0) found = v * E + e;
+      if (now > at) last = v * E + e;
+      at = now;
     }
     return found >= 0 ? found : last;
   };
@@ -679,7 +947,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       unpack<DT>(load_vec<DT>(r.data, v, V), x);
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (v * E + e < V) add(x[e], s, t);
+        add(x[e], s, t);
     }
     double upto = s;
     int upto_t = t;
@@ -731,16 +999,30 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   if (spare_v >= 0 && l.spare == spare_v) finish(walk(spare_v, spare_s, spare_t, INFINITY), total);
 }
 
+// Whether rows are scanned by several workgroups.
+bool sample_splits(int rows, int vocab, int per_vec) { return rows <= 64 && cdiv(vocab, per_vec) > 4096; }
+
 template <int DT>
 void launch(const SampleArgs& a, hipStream_t stream) {
-  const int vectors = cdiv(a.logits.vocab, Elem<DT>::kPerVec);
   const dim3 grid(a.logits.rows);
-  if (vectors <= 4096) sample_kernel<DT, 256><<<grid, dim3(256), 0, stream>>>(a);
-  else if (vectors <= 16384) sample_kernel<DT, 512><<<grid, dim3(512), 0, stream>>>(a);
-  else sample_kernel<DT, 1024><<<grid, dim3(1024), 0, stream>>>(a);
+  const int vectors = cdiv(a.logits.vocab, Elem<DT>::kPerVec);
+  if (sample_splits(a.logits.rows, a.logits.vocab, Elem<DT>::kPerVec)) {
+    scan_kernel<DT><<<dim3(a.logits.rows * kSplit), dim3(kScanThreads), 0, stream>>>(a);
+    sample_kernel<DT, kSplitThreads, true><<<grid, dim3(kSplitThreads), 0, stream>>>(a);
+  } else if (vectors <= 1024 || (vectors <= 4096 && a.logits.rows > a.logits.num_cus)) {
+    sample_kernel<DT, 256, false><<<grid, dim3(256), 0, stream>>>(a);
+  } else if (vectors <= 16384 && a.logits.rows > a.logits.num_cus) {
+    sample_kernel<DT, 512, false><<<grid, dim3(512), 0, stream>>>(a);
+  } else {
+    sample_kernel<DT, 1024, false><<<grid, dim3(1024), 0, stream>>>(a);
+  }
 }
 
 }  // namespace
+
+size_t sample_workspace(int rows, int vocab, int dtype) {
+  return sample_splits(rows, vocab, dtype == RP_LOGITS_F32 ? 4 : 8) ? sizeof(SplitRow) * (size_t)rows : 0;
+}
 
 hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t stream) {
   switch (dtype) {
