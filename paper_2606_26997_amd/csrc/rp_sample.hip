@@ -98,6 +98,38 @@ __device__ inline double pow2(double y) {
 __device__ inline double weight(float x, float ref, double c) {
   return pow2(fmax(((double)x - (double)ref) * c, -1500.0));
 }
+// N at once: their chains of products interleave.
+template <int N>
+__device__ __attribute__((always_inline)) inline void weights(const float (&x)[N], float ref, double c, double (&w)[N]) {
+  constexpr double kRound = 0x1.8p52;
+  constexpr double kPoly[] = {0x1.b63881021ff95p-24, 0x1.63d13637e6ed6p-20, 0x1.ffcb95154c637p-17, 0x1.4308ac85a8c94p-13,
+                              0x1.5d87fe86fea1bp-10, 0x1.3b2ab7181b769p-7,  0x1.c6b08d7047e52p-5,  0x1.ebfbdff823cedp-3,
+                              0x1.62e42fefa39efp-1,  1.0};
+  constexpr int G = 4;
+  static_assert(N % G == 0, "whole groups");
+#pragma unroll
+  for (int g = 0; g < N; g += G) {
+    double f[G], p[G];
+    int n[G];
+#pragma unroll
+    for (int i = 0; i < G; ++i) f[i] = fmax(((double)x[g + i] - (double)ref) * c, -1500.0);
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      const double t = f[i] + kRound;
+      n[i] = __double2loint(t);
+      f[i] -= t - kRound;
+      p[i] = kPoly[0];
+    }
+#pragma unroll
+    for (int k = 1; k < 10; ++k) {
+#pragma unroll
+      for (int i = 0; i < G; ++i) p[i] = fma(p[i], f[i], kPoly[k]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = 0; i < G; ++i) w[g + i] = ldexp(p[i], n[i]);
+  }
+}
 // In steps of 2^-S, scale = 2^S <= 2^50.
 __device__ inline u64 mass_of(double w, double scale) {
   return (u64)__double_as_longlong(fma(w, scale, 0x1p52)) & ((1ull << 52) - 1);
@@ -237,10 +269,11 @@ __device__ __attribute__((always_inline)) inline Scan scan(const Row<DT, NT>& r,
             o.s *= weight(o.ref, most, r.c);
             o.ref = most;
           }
-          double s = weight(x[0], o.ref, r.c);
+          double w[E];
+          weights(x, o.ref, r.c, w);
 #pragma unroll
-          for (int e = 1; e < E; ++e) s += weight(x[e], o.ref, r.c);
-          o.s += s;
+          for (int e = 1; e < E; ++e) w[0] += w[e];
+          o.s += w[0];
         } else {
           const bool more = most > o.top;
           if (more) {
@@ -671,14 +704,16 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       });
       return block_sum<NT>(finite, l.i);
     };
-    // Where the tokens that are kept are many: their number by equal steps of the
-    // logits says which steps the cut lies in (their weights, approximately); then
+    // Where the tokens that are kept are many: their number, or their weight in steps
+    // of 2^-31 of the row's, by equal steps of the logits says which of those the cut
+    // lies in; then
     // one pass sums what is above those steps, by stretch, and lists what is in them.
     // Tokens at `least` and below do not count: LDS would add to one bin for most of
     // a wave. False where that does not settle it.
     const auto wide = [&](bool by_mass, u64 need, float low, uint32_t upper, float least) __attribute__((always_inline)) {
       constexpr int BINS = 2 * kBins;
       uint32_t* counts = reinterpret_cast<uint32_t*>(l.hist);
+      const float c32 = (float)fmin(r.c, 3e38), fine = (float)(0x1p31 / Z);
       const float fit = fmaxf(fminf(r.max - low, 1e30f), 1e-30f), per = (BINS - 2) / fit;
       const auto step = [&](float x) __attribute__((always_inline)) { return BINS - 1 - (int)fminf((r.max - x) * per, BINS - 1.f); };
       __syncthreads();
@@ -687,19 +722,22 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       r.template each<4>(l, upper, [&](int, const float (&x)[E]) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
-          if (x[e] > least) atomicAdd(&counts[step(x[e])], 1u);
+          if (x[e] > least) {
+            // (Whole numbers: LDS adds floats one lane after the other, 192 cycles a wave.)
+            const uint32_t one = by_mass ? (uint32_t)(fast_exp2((x[e] - r.max) * c32) * fine) : 1u;
+            atomicAdd(&counts[step(x[e])], one);
+          }
       });
       __syncthreads();
       const auto value = [&](int bin) __attribute__((always_inline)) {
-        const u64 n = counts[bin];
-        return by_mass && n > 0 ? n * mass_of(weight(r.max - (BINS - 0.5f - bin) / per, r.max, r.c), scale) : n;
+        return by_mass ? (u64)((double)counts[bin] * (0x1p-31 * Z * scale)) : (u64)counts[bin];
       };
       u64 above;
-      const u64 slack = by_mass ? need >> 10 : 0;
-      const int hi = find_top<NT, BINS>(l, need - slack, above, value) + (by_mass ? 1 : 0);
+      const u64 slack = by_mass ? (u64)(Z * scale) >> 14 : 0;  // off by half a step a token at most, and by 32 bits
+      const int hi = find_top<NT, BINS>(l, need > slack ? need - slack : 1, above, value);
       const u64 above_count = above;  // where it is the number of tokens
       __syncthreads();
-      const int lo = by_mass ? find_top<NT, BINS>(l, need + slack, above, value) - 1 : hi;
+      const int lo = by_mass ? find_top<NT, BINS>(l, need + slack, above, value) : hi;
       if (lo <= 0 || (key_q > 0 && step(K::logit(key_q)) > hi)) return false;
       const float edge = r.max - (float)(BINS - lo) / per;
       const uint32_t edge_upper = max(upper, K::upper(K::of(edge - (fabsf(edge) * 1e-5f + fit * 1e-4f))));
@@ -713,11 +751,13 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       double s = 0.0;
       r.template each<4>(l, edge_upper, [&](int v, const float (&x)[E]) {
         uint32_t in = 0;
+        double w[E];
+        weights(x, r.max, r.c, w);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const int at = x[e] > -INFINITY ? step(x[e]) : 0;
-          if (at > hi) s += weight(x[e], r.max, r.c);
-          else if (at >= lo) in |= 1u << e;
+          s += at > hi ? w[e] : 0.0;
+          in |= at >= lo && at <= hi ? 1u << e : 0u;
         }
         for (; in != 0; in &= in - 1) {
           const int i = v * E + __builtin_ctz(in), place = atomicAdd(&l.count, 1);
