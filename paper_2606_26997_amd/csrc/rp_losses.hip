@@ -356,39 +356,41 @@ __global__ __launch_bounds__(threads_of<W>()) void policy_kernel(const PolicyArg
   const double w = a.weights != nullptr ? (double)a.weights[n] : 1.0;
   const bool none = empty || w == 0.0;
   float alpha = 0.f, beta = 0.f, own = 0.f;
-  if (r.id == 0) {
+  if (r.id < 64) {
+    // One wave; its first lanes take an exponential each.
     const double ln_s = log(sums[0]);
     const double lp = empty ? -INFINITY : ((double)at - (double)m) * a.inv_t - ln_s;
     const double H = empty ? 0.0 : ln_s - kLn2_64 * sums[1] / sums[0];
-    const double A = (double)a.advantages[seq];
-    const double ratio = exp(lp - (double)a.old_logprobs[n]);
+    const double A = (double)a.advantages[seq], gap = a.ref_logprobs != nullptr ? (double)a.ref_logprobs[n] - lp : 0.0;
+    const double e = exp(r.id == 0 ? lp - (double)a.old_logprobs[n] : r.id == 1 ? gap : lp);
+    const double ratio = __shfl(e, 0), e_gap = __shfl(e, 1), p = __shfl(e, 2);
+    // 1 - p, also where lp is small: -lp - lp^2 / 2 - lp^3 / 6 is 4e-14 off at 1e-4.
+    const double not_p = lp > -1e-4 ? -lp * (1.0 + lp * (0.5 + lp * (1.0 / 6.0))) : 1.0 - p;
     const double free_s = ratio * A, held = fmin(fmax(ratio, 1.0 - a.clip_low), 1.0 + a.clip_high) * A;
     // Written so that a NaN on either side stays one.
     const bool is_free = !(held < free_s);
     double loss = -(is_free ? free_s : held) - a.entropy_coef * H, g = is_free ? -free_s : 0.0;
     if (a.ref_logprobs != nullptr) {
-      const double gap = (double)a.ref_logprobs[n] - lp, e = exp(gap);
-      loss += a.kl_beta * (e - gap - 1.0);
-      g += a.kl_beta * (1.0 - e);
+      loss += a.kl_beta * (e_gap - gap - 1.0);
+      g += a.kl_beta * (1.0 - e_gap);
     }
-    a.losses[n] = none ? 0.f : (float)(w * loss);
-    if (a.logprobs != nullptr) a.logprobs[n] = (float)lp;
-    if (a.entropy != nullptr) a.entropy[n] = (float)H;
+    if (r.id == 0) {
+      a.losses[n] = none ? 0.f : (float)(w * loss);
+      if (a.logprobs != nullptr) a.logprobs[n] = (float)lp;
+      if (a.entropy != nullptr) a.entropy[n] = (float)H;
+    }
     // d loss / d x_i = w / T (g ([i = y] - p_i) + b p_i (ln p_i + H)), ln p_i = d_i ln 2 - ln S.
-    const double per = w * a.inv_t, b = a.entropy_coef, p = exp(lp);
+    const double per = w * a.inv_t, b = a.entropy_coef;
     alpha = (float)(per * (b * (H - ln_s) - g) / sums[0]);
     beta = (float)(per * b * kLn2_64 / sums[0]);
-    own = (float)(per * (-g * expm1(lp) + (b != 0.0 && p > 0.0 ? b * p * (lp + H) : 0.0)));
+    own = (float)(per * (g * not_p + (b != 0.0 && p > 0.0 ? b * p * (lp + H) : 0.0)));
   }
   if constexpr (GRAD) {
     if (none) {
       r.zero(out);
       return;
     }
-    if constexpr (W == 1) {
-      alpha = __shfl(alpha, 0);
-      beta = __shfl(beta, 0);
-    } else {
+    if constexpr (W > 1) {
       if (r.id == 0) {
         slots.out[0] = alpha;
         slots.out[1] = beta;
@@ -409,8 +411,10 @@ __global__ __launch_bounds__(threads_of<W>()) void policy_kernel(const PolicyArg
 // Entry j < k of a row's list counts where its id is in the vocabulary, is not
 // listed before it and its value is above -inf.
 struct Entry {
-  int id;  // -1: does not count
-  float value, x, grad;
+  int id;    // -1: does not count
+  float x;   // its logit, then its gradient
+  double e;  // of the student (not divided by S)
+  double t;  // the teacher's value, then, but for REVERSE, its probability (TOPK: not divided by their sum)
 };
 
 // Words of the bits, with those of the vectors that no row has (a team's threads
@@ -421,7 +425,7 @@ template <int DT, int W, int NV, bool GRAD>
 __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillArgs a) {
   static_assert(W > 1, "a workgroup per row");
   __shared__ Slots<W> slots;
-  extern __shared__ char dynamic[];
+  extern __shared__ __align__(16) char dynamic[];
   constexpr int NT = W * 64, E = Elem<DT>::kPerVec;
   const int V = a.logits.vocab, K = a.k, tid = threadIdx.x;
   Entry* list = reinterpret_cast<Entry*>(dynamic);
@@ -451,7 +455,7 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
     const float value = a.values[(long long)n * K + j];
     if ((unsigned)id >= (unsigned)V || value == -INFINITY) id = -1;
     list[j].id = id;
-    list[j].value = value;
+    list[j].t = (double)value;
     if (id < 0) continue;
     list[j].x = Elem<DT>::get(row, id);
     const int bit = bit_of(id);
@@ -477,7 +481,7 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
   for (int j = tid; j < K; j += NT) {
     if (list[j].id < 0) continue;
     top = fmaxf(top, list[j].x);
-    tm = fmaxf(tm, list[j].value);
+    tm = fmaxf(tm, (float)list[j].t);
   }
   // Sums over the tokens outside the list; those of the list are added apart,
   // so that a small mass outside is no difference of large ones.
@@ -501,8 +505,10 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
   for (int j = tid; j < K; j += NT) {
     if (list[j].id < 0) continue;
     const double z = ((double)list[j].x - (double)m) * a.inv_t, e = exp(z);
-    const double t = a.kind == RP_DISTILL_TOPK ? ((double)list[j].value - (double)tm) * a.inv_t : (double)list[j].value;
+    const double t = a.kind == RP_DISTILL_TOPK ? (list[j].t - (double)tm) * a.inv_t : list[j].t;
     const double P = exp(t);
+    list[j].e = e;
+    if (a.kind != RP_DISTILL_REVERSE) list[j].t = P;
     sums[1] += e;
     sums[2] += P;
     if (a.kind == RP_DISTILL_REVERSE) sums[3] += e == 0.0 ? 0.0 : e * (z - t);
@@ -529,12 +535,12 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
   if (tid == 0) a.losses[n] = empty ? 0.f : (float)((double)w * loss);
   for (int j = tid; GRAD && j < K; j += NT) {
     if (list[j].id < 0) continue;
-    const double z = ((double)list[j].x - (double)m) * a.inv_t, q = exp(z) / s, t = (double)list[j].value;
+    const double q = list[j].e / s;
     double g;
-    if (a.kind == RP_DISTILL_TOPK) g = q - exp((t - (double)tm) * a.inv_t) / P_sum;
-    else if (a.kind == RP_DISTILL_TAIL) g = whole * q - exp(t);
-    else g = q == 0.0 ? 0.0 : q * (z - ln_s - t - loss);
-    list[j].grad = (float)(per * g);
+    if (a.kind == RP_DISTILL_TOPK) g = q - list[j].t / P_sum;
+    else if (a.kind == RP_DISTILL_TAIL) g = whole * q - list[j].t;
+    else g = q == 0.0 ? 0.0 : q * (((double)list[j].x - (double)m) * a.inv_t - ln_s - list[j].t - loss);
+    list[j].x = (float)(per * g);
   }
   if constexpr (GRAD) {
     if (empty) {
@@ -545,7 +551,7 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
     r.store(row, out, [&](float x) { return fast_exp2((x - m) * c) * alpha; });
     __syncthreads();  // the list's elements come after their vectors
     for (int j = tid; j < K; j += NT)
-      if (list[j].id >= 0) put_elem<DT>(out, list[j].id, list[j].grad);
+      if (list[j].id >= 0) put_elem<DT>(out, list[j].id, list[j].x);
   }
 }
 
@@ -555,11 +561,14 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
 // the other loads or stores (policy loss of 2048 rows of 151936 bf16 logits: 262
 // us; sixteen waves, one row to a unit, 280; held whole in sixteen waves'
 // registers, where every unit computes at the same time, 382); sixteen where
-// there are too few rows for that (512 rows of 151936 fp32 logits: 139 us, 145).
+// there are too few rows for that (512 rows of 151936 fp32 logits: 139 us, 145;
+// 24 rows of 32000 bf16: @@).
 template <int DT>
 int waves_of(const LogitArgs& l) {
   const int vectors = cdiv(l.vocab, Elem<DT>::kPerVec);
-  return vectors <= 1024 ? 1 : vectors <= 4096 ? 4 : l.rows > 2 * l.num_cus ? 8 : 16;
+  if (vectors <= 1024) return 1;
+  if (vectors <= 4096) return l.rows > l.num_cus ? 4 : 16;
+  return l.rows > 2 * l.num_cus ? 8 : 16;
 }
 
 template <int DT>
