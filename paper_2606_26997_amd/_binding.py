@@ -448,34 +448,58 @@ def kv_write_slots(kv, slot_map, k_new, v_new, src_rows=None, stream=None) -> No
                                     rows, _stream(stream)), "rp_kv_write_slots")
 
 
-def _rows(name, t, like=None):
-    """(rows, vocab, stride) of a [rows][vocab] tensor whose rows are contiguous; `like`: of that one's shape, dtype
-    and device."""
+def _rows(name, t, device, like=None):
+    """Rows, vocabulary and row stride of a [rows][vocab] tensor on the GPU `device` whose rows are contiguous; `like`:
+    of that one's shape and dtype."""
     if t.dtype not in RP_LOGITS_DTYPES or (like is not None and t.dtype is not like.dtype):
         raise ValueError(f"{name}: dtype {t.dtype}, not "
                          f"{'bfloat16, float16 or float32' if like is None else like.dtype}")
     if t.dim() != 2 or (like is not None and t.shape != like.shape):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, not {'[rows][vocab]' if like is None else tuple(like.shape)}")
     n, v = t.shape
-    if v > 1 and t.stride(1) != 1:
+    stride, one = t.stride()
+    if one != 1 and v > 1:
         raise ValueError(f"{name}: the logits of a row must be contiguous (strides {t.stride()})")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    if t.get_device() != device or device < 0:
         raise ValueError(f"{name} is on {t.device}, not on the current GPU")
-    stride = t.stride(0) if n > 1 else v
-    if stride < v:
+    if n <= 1:
+        stride = v
+    elif stride < v:
         raise ValueError(f"{name}: rows overlap (strides {t.stride()})")
     return n, v, stride
 
 
-def _logits(t) -> RpLogits:
-    n, v, stride = _rows("logits", t)
+def _device() -> int:
+    return torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else -1
+
+
+def _logits(t, device) -> RpLogits:
+    n, v, stride = _rows("logits", t, device)
     return RpLogits(t.data_ptr(), n, v, stride, RP_LOGITS_DTYPES[t.dtype])
+
+
+def _per_row(n, device, *specs) -> None:
+    """_tensors for arrays of n entries, (name, tensor, dtype), None among them: what is fine passes quickly."""
+    shape = (n,)
+    for name, t, dtype in specs:
+        if t is not None and (isinstance(t, int) or t.dtype is not dtype or t.shape != shape or t.get_device() != device
+                              or not t.is_contiguous()):
+            _tensors((name, t, dtype, shape))
+
+
+def _work_ptr(workspace, device):
+    if workspace is None or isinstance(workspace, int):
+        return workspace
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        _tensors(("workspace", workspace, None, None))
+    return workspace.data_ptr()
 
 
 def logits_workspace_size(logits) -> int:
     """Bytes of workspace that any of the calls on these logits ([rows][vocab], bf16, fp16 or fp32) needs."""
     n = ctypes.c_size_t(0)
-    _check(load().rp_logits_workspace_size(ctypes.byref(_logits(logits)), ctypes.byref(n)), "rp_logits_workspace_size")
+    _check(load().rp_logits_workspace_size(ctypes.byref(_logits(logits, _device())), ctypes.byref(n)),
+           "rp_logits_workspace_size")
     return int(n.value)
 
 
@@ -483,27 +507,27 @@ def sample_tokens(logits, u, tokens, logprobs=None, kept_logprobs=None, *, tempe
                   min_p=None, workspace=None, stream=None) -> None:
     """Draw tokens (int32 [rows]) from logits [rows][vocab] with the uniform numbers u (fp32 [rows]); logprobs and
     kept_logprobs fp32 [rows] or None. temperature, top_p, min_p: fp32 [rows]; top_k: int32 [rows]; None for none."""
-    l, f32 = _logits(logits), torch.float32
-    row = (l.num_rows,)
-    _tensors(("u", u, f32, row), ("tokens", tokens, torch.int32, row), ("logprobs", logprobs, f32, row),
-             ("kept_logprobs", kept_logprobs, f32, row), ("temperature", temperature, f32, row),
-             ("top_k", top_k, torch.int32, row), ("top_p", top_p, f32, row), ("min_p", min_p, f32, row),
-             ("workspace", workspace, None, None))
+    device, f32 = _device(), torch.float32
+    l = _logits(logits, device)
+    _per_row(l.num_rows, device, ("u", u, f32), ("tokens", tokens, torch.int32), ("logprobs", logprobs, f32),
+             ("kept_logprobs", kept_logprobs, f32), ("temperature", temperature, f32), ("top_k", top_k, torch.int32),
+             ("top_p", top_p, f32), ("min_p", min_p, f32))
     how = RpSampling(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
     _check(load().rp_sample_tokens(ctypes.byref(l), ctypes.byref(how), _ptr(u), _ptr(tokens), _ptr(logprobs),
-                                   _ptr(kept_logprobs), _ptr(workspace), _ws_bytes(workspace), _stream(stream)),
+                                   _ptr(kept_logprobs), _work_ptr(workspace, device), _ws_bytes(workspace),
+                                   _stream(stream)),
            "rp_sample_tokens")
 
 
 def token_logprobs(logits, tokens, logprobs, entropy=None, *, temperature=1.0, workspace=None, stream=None) -> None:
     """Log-probabilities (fp32 [rows]) of tokens (int32 [rows]; others than 0 .. vocab-1 are skipped) in logits
     [rows][vocab], and the rows' entropies (fp32 [rows] or None)."""
-    l = _logits(logits)
-    row = (l.num_rows,)
-    _tensors(("tokens", tokens, torch.int32, row), ("logprobs", logprobs, torch.float32, row),
-             ("entropy", entropy, torch.float32, row), ("workspace", workspace, None, None))
+    device = _device()
+    l = _logits(logits, device)
+    _per_row(l.num_rows, device, ("tokens", tokens, torch.int32), ("logprobs", logprobs, torch.float32),
+             ("entropy", entropy, torch.float32))
     _check(load().rp_token_logprobs(ctypes.byref(l), _ptr(tokens), float(temperature), _ptr(logprobs), _ptr(entropy),
-                                    _ptr(workspace), _ws_bytes(workspace), _stream(stream)), "rp_token_logprobs")
+                                    _work_ptr(workspace, device), _ws_bytes(workspace), _stream(stream)), "rp_token_logprobs")
 
 
 def policy_loss(logits, tokens, old_logprobs, advantages, losses, dlogits=None, *, row_seq=None, weights=None,
@@ -513,20 +537,19 @@ def policy_loss(logits, tokens, old_logprobs, advantages, losses, dlogits=None, 
     it may be the logits), the gradient of their sum. tokens, row_seq: int32 [rows]; advantages: fp32, of any shape,
     entry row_seq[n] for row n (n without row_seq); old_logprobs, ref_logprobs, weights, logprobs, entropy: fp32
     [rows]. Rows whose token or row_seq is out of range are skipped."""
-    l, f32 = _logits(logits), torch.float32
-    row = (l.num_rows,)
-    _tensors(("tokens", tokens, torch.int32, row), ("old_logprobs", old_logprobs, f32, row),
-             ("advantages", advantages, f32, None), ("losses", losses, f32, row),
-             ("row_seq", row_seq, torch.int32, row), ("weights", weights, f32, row),
-             ("ref_logprobs", ref_logprobs, f32, row), ("logprobs", logprobs, f32, row),
-             ("entropy", entropy, f32, row), ("workspace", workspace, None, None))
-    stride = _rows("dlogits", dlogits, logits)[2] if dlogits is not None else 0
+    device, f32 = _device(), torch.float32
+    l = _logits(logits, device)
+    _per_row(l.num_rows, device, ("tokens", tokens, torch.int32), ("old_logprobs", old_logprobs, f32),
+             ("losses", losses, f32), ("row_seq", row_seq, torch.int32), ("weights", weights, f32),
+             ("ref_logprobs", ref_logprobs, f32), ("logprobs", logprobs, f32), ("entropy", entropy, f32))
+    _tensors(("advantages", advantages, f32, None))
+    stride = _rows("dlogits", dlogits, device, logits)[2] if dlogits is not None else 0
     batch = RpPolicyBatch(_ptr(tokens), _ptr(old_logprobs), _ptr(ref_logprobs), _ptr(advantages), _ptr(row_seq),
                           advantages.numel(), _ptr(weights), float(temperature), float(clip_low), float(clip_high),
                           float(kl_beta), float(entropy_coef))
     _check(load().rp_policy_loss(ctypes.byref(l), ctypes.byref(batch), _ptr(losses), _ptr(logprobs), _ptr(entropy),
-                                 _ptr(dlogits), stride, _ptr(workspace), _ws_bytes(workspace), _stream(stream)),
-           "rp_policy_loss")
+                                 _ptr(dlogits), stride, _work_ptr(workspace, device), _ws_bytes(workspace),
+                                 _stream(stream)), "rp_policy_loss")
 
 
 def distill_loss(logits, ids, values, losses, dlogits=None, *, kind="tail", weights=None, temperature=1.0,
@@ -536,15 +559,16 @@ def distill_loss(logits, ids, values, losses, dlogits=None, *, kind="tail", weig
     RP_DISTILL_KINDS; weights fp32 [rows] or None."""
     if kind not in RP_DISTILL_KINDS:
         raise ValueError(f"kind {kind!r}, not one of {', '.join(RP_DISTILL_KINDS)}")
-    l, f32 = _logits(logits), torch.float32
-    _tensors(("ids", ids, torch.int32, (l.num_rows, None)), ("values", values, f32, (l.num_rows, ids.shape[1])),
-             ("losses", losses, f32, (l.num_rows,)), ("weights", weights, f32, (l.num_rows,)),
-             ("workspace", workspace, None, None))
-    stride = _rows("dlogits", dlogits, logits)[2] if dlogits is not None else 0
+    device, f32 = _device(), torch.float32
+    l = _logits(logits, device)
+    _tensors(("ids", ids, torch.int32, (l.num_rows, None)), ("values", values, f32, (l.num_rows, ids.shape[1])))
+    _per_row(l.num_rows, device, ("losses", losses, f32), ("weights", weights, f32))
+    stride = _rows("dlogits", dlogits, device, logits)[2] if dlogits is not None else 0
     teacher = RpTeacher(_ptr(ids), _ptr(values), ids.shape[1], RP_DISTILL_KINDS[kind], _ptr(weights),
                         float(temperature))
     _check(load().rp_distill_loss(ctypes.byref(l), ctypes.byref(teacher), _ptr(losses), _ptr(dlogits), stride,
-                                  _ptr(workspace), _ws_bytes(workspace), _stream(stream)), "rp_distill_loss")
+                                  _work_ptr(workspace, device), _ws_bytes(workspace), _stream(stream)),
+           "rp_distill_loss")
 
 
 def prefill_layout(prompt_offs, prefix_block_table, *, num_q_heads, num_tokens) -> RpPrefillLayout:
