@@ -197,7 +197,7 @@ struct How {
   int k;        // vocab: all
   double p, q;  // 1 and 0: all
   double inv_t;
-  bool all, exact, light;  // exact: a border hangs on the row's whole sum; light: k few enough for a list
+  bool all, light;  // all: a border hangs on every token's weight; light: k few enough for a list
   __device__ inline How(const SampleArgs& a, int n, int lightest) {
     const int V = a.logits.vocab;
     const float T = a.temperature != nullptr ? a.temperature[n] : 1.f;
@@ -211,7 +211,6 @@ struct How {
     inv_t = greedy ? 1.0 : fmax(1.0 / (double)T, 1e-300);
     light = k < V && k <= lightest;
     all = k >= V && p >= 1.0 && q == 0.0;
-    exact = k >= V && (p < 1.0 || q == 0.0);
   }
 };
 
@@ -339,11 +338,11 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(const SampleArgs a) 
   const How how(a, n, kSplitThreads / 2);
   r.c = kLog2e64 * how.inv_t;
   const int thread = stretch * 64 + tid % 64;
-  const Scan o = scan(r, thread, tid / 64, kScanThreads / 64, how.exact,
+  const Scan o = scan(r, thread, tid / 64, kScanThreads / 64, how.all,
                       [&](int g, uint16_t key) { out.top[g * kSplitThreads + thread] = key; });
   const float top = block_max<kScanThreads>(o.top, lds_f);
   const bool bad = __syncthreads_or(o.bad);
-  const double s = block_sum<kScanThreads>(bad ? 0.0 : sum_to(o, r, top, how.exact), lds_d);
+  const double s = block_sum<kScanThreads>(bad ? 0.0 : sum_to(o, r, top, how.all), lds_d);
   if (tid == 0) out.part[stretch] = {top, bad ? 1 : 0, s};
 }
 
@@ -489,7 +488,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     r.max = wave_max(part.top);
     bad = __ballot(part.bad != 0) != 0;
     if (tid < kSplit && part.top > -INFINITY)
-      l.d[tid] = part.s * (how.exact ? weight(part.top, r.max, r.c)
+      l.d[tid] = part.s * (how.all ? weight(part.top, r.max, r.c)
                                      : (double)fast_exp2((part.top - r.max) * (float)fmin(r.c, 3e38)));
     else if (tid < kSplit) l.d[tid] = 0.0;
     uint32_t most = 0;
@@ -501,12 +500,12 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     const uint32_t o = most << 16;
     if (most > 0x007Fu) top = __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
   } else {
-    const Scan o = scan(r, tid, 0, 1, how.exact, [&](int g, uint16_t key) { l.top[g * NT + tid] = key; });
+    const Scan o = scan(r, tid, 0, 1, how.all, [&](int g, uint16_t key) { l.top[g * NT + tid] = key; });
     top = o.top;
     r.max = block_max<NT>(top, l.f);
     bad = __syncthreads_or(o.bad);
     if (!bad && r.max > -INFINITY) {
-      const double s = wave_sum(sum_to(o, r, r.max, how.exact));
+      const double s = wave_sum(sum_to(o, r, r.max, how.all));
       if (lane == 0) l.d[wave] = s;
     }
   }
@@ -569,7 +568,12 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     };
     const uint32_t most = K::of(r.max);
     const bool probe = k >= V && p < 1.0;
-    const u64 need_p = (u64)fmax(ceil(p * Z * scale), 1.0);  // where every token counts
+    // The mass of the nucleus, where every token counts, for which Z in 32 bits leaves
+    // a range: a term is off by (3 |d| + 2) 2^-24, |d| ln 2 averages at most ln V < 14,
+    // and a thread adds `steps` of them, in vectors of 8.
+    const double off = (128.0 + r.steps) * 0x1p-24;
+    const u64 need_lo = (u64)fmax(ceil(p * Z * (1.0 - off) * scale), 1.0);
+    const u64 need_hi = max((u64)ceil(p * Z * (1.0 + off) * scale), need_lo);
     uint32_t key_q = 0;  // the least key of weight q or more
     if (q > 0.0) {
       const double least = (double)r.max + log2(q) / r.c;
@@ -579,14 +583,14 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     }
     uint32_t tau = 0;
     if (light_k) tau = max(reached(false, (u64)k), K::kNegInf + 1);
-    else if (probe) tau = reached(true, need_p);
+    else if (probe) tau = reached(true, need_hi);
     else if (k >= V) tau = key_q;
     if (tau != 0)
       listed = gather(l, r, tau, scale);
 
     // A short list: every token counts those before it, in the order of keys and in
     // that of indices, the waves sharing out whom they count.
-    if (listed && l.count <= Lds<NT>::kSmall) {
+    while (listed && l.count <= Lds<NT>::kSmall) {
       const int count = l.count, blocks = cdiv(count, 64), shares = kWaves / blocks;
       const int at = wave % blocks * 64 + lane, share = wave / blocks;
       const int from = share * count / shares, to = share < shares ? (share + 1) * count / shares : from;
@@ -616,9 +620,14 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       const Token mine = is ? l.list[tid] : Token{0, 0};
       bool in = is && l.rank[tid] < k;
       if (p < 1.0) {
-        u64 need = need_p;
+        u64 need = need_lo;
         if (k < V) need = (u64)fmax(ceil(p * (double)block_sum<NT>(in ? mine.mass : 0, l.q)), 1.0);
-        in = in && l.over[tid] < need;
+        const bool kept = in && l.over[tid] < need;
+        if (probe && __syncthreads_or(in && !kept && l.over[tid] < need_hi)) {
+          listed = false;  // Z in 32 bits does not tell
+          break;
+        }
+        in = kept;
       }
       in = in && mine.key() >= key_q;
       const u64 mass = in ? mine.mass : 0, sum = block_sum<NT>(mass, l.q);
@@ -710,7 +719,9 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     // one pass sums what is above those steps, by stretch, and lists what is in them.
     // Tokens at `least` and below do not count: LDS would add to one bin for most of
     // a wave. False where that does not settle it.
-    const auto wide = [&](bool by_mass, u64 need, float low, uint32_t upper, float least) __attribute__((always_inline)) {
+    bool settled = false;  // cut and ties are known
+    bool whole_sum = false;  // Z is the sum in 64 bits
+    const auto wide = [&](bool by_mass, u64 from, u64 to, float low, uint32_t upper, float least) __attribute__((always_inline)) {
       constexpr int BINS = 2 * kBins;
       uint32_t* counts = reinterpret_cast<uint32_t*>(l.hist);
       const float c32 = (float)fmin(r.c, 3e38), fine = (float)(0x1p31 / Z);
@@ -724,7 +735,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
         for (int e = 0; e < E; ++e)
           if (x[e] > least) {
             // (Whole numbers: LDS adds floats one lane after the other, 192 cycles a wave.)
-            const uint32_t one = by_mass ? (uint32_t)(fast_exp2((x[e] - r.max) * c32) * fine) : 1u;
+            const uint32_t one = by_mass ? (uint32_t)fmaf(fast_exp2((x[e] - r.max) * c32), fine, 0.5f) : 1u;
             atomicAdd(&counts[step(x[e])], one);
           }
       });
@@ -733,14 +744,21 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
         return by_mass ? (u64)((double)counts[bin] * (0x1p-31 * Z * scale)) : (u64)counts[bin];
       };
       u64 above;
-      const u64 slack = by_mass ? (u64)(Z * scale) >> 14 : 0;  // off by half a step a token at most, and by 32 bits
-      const int hi = find_top<NT, BINS>(l, need > slack ? need - slack : 1, above, value);
+      const u64 slack = by_mass ? (u64)(Z * scale * (V * 0x1p-32 + off)) : 0;  // half a step a token, and Z's
+      const int hi = find_top<NT, BINS>(l, from > slack ? from - slack : 1, above, value);
       const u64 above_count = above;  // where it is the number of tokens
       __syncthreads();
-      const int lo = by_mass ? find_top<NT, BINS>(l, need + slack, above, value) : hi;
-      if (lo <= 0 || (key_q > 0 && step(K::logit(key_q)) > hi)) return false;
+      const int lo = by_mass ? find_top<NT, BINS>(l, to + slack, above, value) : hi;
+      if (lo <= 0) return false;
+      if (key_q > 0 && step(K::logit(key_q)) > hi) {
+        cut = key_q;
+        ties = V;
+        settled = true;
+        return false;
+      }
       const float edge = r.max - (float)(BINS - lo) / per;
-      const uint32_t edge_upper = max(upper, K::upper(K::of(edge - (fabsf(edge) * 1e-5f + fit * 1e-4f))));
+      // Z is summed on the way, over every vector.
+      const uint32_t edge_upper = by_mass ? 0 : max(upper, K::upper(K::of(edge - (fabsf(edge) * 1e-5f + fit * 1e-4f))));
       __syncthreads();
       if (tid == 0) {
         l.count = 0;
@@ -748,7 +766,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
         l.most = 0;
       }
       __syncthreads();
-      double s = 0.0;
+      double s = 0.0, others = 0.0;
       r.template each<4>(l, edge_upper, [&](int v, const float (&x)[E]) {
         uint32_t in = 0;
         double w[E];
@@ -757,6 +775,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
         for (int e = 0; e < E; ++e) {
           const int at = x[e] > -INFINITY ? step(x[e]) : 0;
           s += at > hi ? w[e] : 0.0;
+          others += at > hi ? 0.0 : w[e];
           in |= at >= lo && at <= hi ? 1u << e : 0u;
         }
         for (; in != 0; in &= in - 1) {
@@ -772,10 +791,17 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       s = wave_sum(s);
       if (lane == 0) l.d[wave] = s;
       __syncthreads();
-      if (l.count > Lds<NT>::kList || l.count == 0) return false;
       double over = 0.0;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) over += l.d[w];
+      u64 need = from;
+      if (by_mass) {
+        double* sums = reinterpret_cast<double*>(l.q);
+        Z = over + block_sum<NT>(others, sums);
+        whole_sum = true;
+        need = (u64)fmax(ceil(p * Z * scale), 1.0);
+      }
+      if (l.count > Lds<NT>::kList || l.count == 0) return false;
       u64 sum = 0;
       from_list([&](uint32_t, uint32_t, u64 mass) { sum += by_mass ? mass : 1; });
       sum = block_sum<NT>(sum, l.q);
@@ -809,14 +835,33 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       __syncthreads();
       return true;
     };
-    if (!listed && probe) {
-      // Tokens of less than (1 - p) Z / V each sum to less than (1 - p) Z: none of them is in the nucleus.
-      const float low = fmaxf((float)((double)r.max + log2((1.0 - p) * Z / V) / r.c), -3e38f);
-      const float slack = fabsf(low) * 1e-5f + (r.max - low) * 1e-5f;
-      const bool sure = low > -3e38f;
-      summed = wide(true, need_p, low, sure ? K::upper(K::of(low - slack)) : 0, sure ? low - slack : -INFINITY);
+    const auto set_cut = [&](const Cut& found, u64 need) __attribute__((always_inline)) {
+      const u64 each = mass_of(weight(K::logit(found.key), r.max, r.c), scale);
+      const u64 rest = need > found.above ? need - found.above : 1;
+      const u64 some = each > 0 ? (rest + each - 1) / each : (u64)V;
+      if (found.key > cut || (found.key == cut && ties > 0)) {
+        ties = found.key > cut ? (int)min(some, (u64)V) : min(ties, (int)min(some, (u64)V));
+        cut = found.key;
+      }
+      return found.above + some * each;
+    };
+    if (probe && listed) {
+      const Cut found = descend(l, K::kNegInf + 1, most, need_lo, [&](auto&& f) {
+        from_list([&](uint32_t key, uint32_t, u64 mass) { f(key, mass); });
+      });
+      listed = settled = set_cut(found, need_lo) >= need_hi;  // else Z in 32 bits does not tell
+    }
+    // Tokens of less than (1 - p) Z / V each sum to less than (1 - p) Z: none of them is in the nucleus.
+    const float low = probe ? fmaxf((float)((double)r.max + log2((1.0 - p) * Z * (1.0 - off) / V) / r.c), -3e38f) : 0.f;
+    const float low_slack = fabsf(low) * 1e-5f + (r.max - low) * 1e-5f;
+    const bool sure = probe && low > -3e38f;
+    const uint32_t low_upper = sure ? K::upper(K::of(low - low_slack)) : 0;
+    if (probe && !listed) {
+      cut = K::kNegInf;
+      ties = 0;
+      summed = wide(true, need_lo, need_hi, low, low_upper, sure ? low - low_slack : -INFINITY);
     } else if (!listed && k < V && p >= 1.0 && tokens_at_all() > k) {
-      summed = wide(false, (u64)k, r.max - 2.f * (r.max - least_top), 0, -INFINITY);
+      summed = wide(false, (u64)k, (u64)k, r.max - 2.f * (r.max - least_top), 0, -INFINITY);
     }
 
     u64 kept_mass = 0;  // of the top-k tokens
@@ -852,27 +897,24 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
         if (ties > 0) kept_mass += (u64)ties * mass_of(weight(K::logit(cut), r.max, r.c), scale);
       }
     }
-    if (p < 1.0 && !summed) {
-      const u64 need = k < V ? (u64)fmax(ceil(p * (double)kept_mass), 1.0) : need_p;
-      Cut found;
-      if (listed) {
-        found = descend(l, K::kNegInf + 1, most, need, [&](auto&& f) {
-          from_list([&](uint32_t key, uint32_t, u64 mass) { f(key, mass); });
+    if (p < 1.0 && !summed && !settled) {
+      if (probe && !whole_sum) {
+        double s = 0.0;
+        r.template each<1>(l, 0, [&](int, const float (&x)[E]) {
+          double w[E];
+          weights(x, r.max, r.c, w);
+#pragma unroll
+          for (int e = 0; e < E; ++e) s += w[e];
         });
-      } else {
-        // Tokens of less than (1 - p) Z / V each sum to less than (1 - p) Z: none of them is in the nucleus.
-        const float low = (float)((double)r.max + log2((1.0 - p) * Z / V) / r.c);
-        const float slack = fabsf(low) * 1e-5f + (r.max - low) * 1e-5f;
-        const bool sure = probe && low > -3e38f;
-        found = from_row(false, need, fmaxf(low, -3e38f), sure ? K::upper(K::of(low - slack)) : 0);
-        listed = false;
+        Z = block_sum<NT>(s, l.d);
       }
-      const u64 each = mass_of(weight(K::logit(found.key), r.max, r.c), scale);
-      const u64 rest = need > found.above ? need - found.above : 1;
-      const u64 some = each > 0 ? (rest + each - 1) / each : (u64)V;
-      if (found.key > cut || (found.key == cut && ties > 0)) {
-        ties = found.key > cut ? (int)min(some, (u64)V) : min(ties, (int)min(some, (u64)V));
-        cut = found.key;
+      const u64 need = (u64)fmax(ceil(p * (k < V ? (double)kept_mass : Z * scale)), 1.0);
+      if (listed) {
+        set_cut(descend(l, K::kNegInf + 1, most, need, [&](auto&& f) {
+          from_list([&](uint32_t key, uint32_t, u64 mass) { f(key, mass); });
+        }), need);
+      } else {
+        set_cut(from_row(false, need, probe ? low : r.max - 2.f * (r.max - least_top), low_upper), need);
       }
     }
     if (key_q > cut && !summed) {
