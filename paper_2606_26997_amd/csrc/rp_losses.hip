@@ -32,9 +32,11 @@ struct Stats {
   int at = -1;
 };
 
-// About 11 instructions a logit (of 4 for the exponential), 14 with a running
-// maximum and differences x - m: 8192 rows of 151936 bf16 logits take 470 us that
-// way, where the vector units are busy for 443.
+// Five vector operations a logit, of 2 cycles each but the exponential's 8, and two
+// of a conversion and of the maximum: with a reference that moved with every maximum,
+// and so differences x - m, log-probabilities of 8192 rows of 151936 bf16 logits took
+// 470 us and the vector units were the bound; 437 this way, 425 with the loads past
+// the caches (5.9 TB/s).
 template <int E>
 __device__ inline void add_values(Stats& a, int v, const float (&x)[E], float c) {
   float top = x[0];
@@ -94,12 +96,8 @@ template <int W>
 struct Slots {
   float m[W];
   double d[W][5];
-  float out[4];
+  float out[3];
 };
-template <int W>
-__device__ inline void team_barrier() {
-  if constexpr (W > 1) __syncthreads();
-}
 template <int W>
 __device__ inline float team_max(float x, Slots<W>& s) {
   x = wave_max(x);
@@ -141,7 +139,7 @@ constexpr int threads_of() {
 // vector, one per thread. Row pointers are the same for a whole wave, so that an
 // access is a scalar base, one offset register and no more. (Vectors from the
 // row's start, off the boundary: distillation of 1500 rows of 100003 fp16 logits
-// 177 us, 160 this way.)
+// 177 us, 155 this way.)
 template <int DT, int W, int NV>
 struct Row {
   static constexpr int E = Elem<DT>::kPerVec, NT = W * 64, kHeld = NV > 0 ? NV : 1;
@@ -155,9 +153,13 @@ struct Row {
     whole = (vocab - head) / E;
     loose = vocab - whole * E;
   }
-  // The token of vector v's first logit, and of the thread's loose one.
-  __device__ inline int first_of(int v) const { return head + v * E; }
+  // The thread's loose token.
   __device__ inline int loose_of() const { return id < head ? id : whole * E + id; }
+  // The thread that has a token.
+  __device__ inline int owner_of(int token) const {
+    const int v = token - head;
+    return v < 0 ? token : v < whole * E ? v / E % NT : token - whole * E;
+  }
 
   // Vector j of the thread; threads behind the last whole vector read that one. What
   // is read once (ONCE) goes past the caches (log-probabilities of 1024 rows of 151936
@@ -172,9 +174,8 @@ struct Row {
   __device__ inline void put(char* out, int j, const float (&x)[E]) const {
     u32x4_any* at =
         reinterpret_cast<u32x4_any*>(out + head * Elem<DT>::kBytes + (size_t)j * (NT * 16) + (uint32_t)id * 16u);
-    // Rows that are not held are read again from the caches: their gradients go past those.
-    if constexpr (W >= 8) __builtin_nontemporal_store(pack<DT>(x), at);
-    else *at = pack<DT>(x);
+    // Past the caches (4096 rows of 32000 bf16 logits: 107 us, 102 this way).
+    __builtin_nontemporal_store(pack<DT>(x), at);
   }
   __device__ inline void fetch_all(const char* row) {
 #pragma unroll
@@ -336,7 +337,6 @@ __global__ __launch_bounds__(threads_of<W>()) void logprobs_kernel(const Logprob
 template <int DT, int W, int NV, bool GRAD>
 __global__ __launch_bounds__(threads_of<W>()) void policy_kernel(const PolicyArgs a) {
   __shared__ Slots<W> slots;
-  constexpr int E = Elem<DT>::kPerVec;
   const int n = W == 1 ? blockIdx.x * 4 + wave_id() : blockIdx.x, V = a.logits.vocab;
   if (n >= a.logits.rows) return;
   const char* row = row_of<DT>(a.logits, n);
@@ -399,17 +399,19 @@ __global__ __launch_bounds__(threads_of<W>()) void policy_kernel(const PolicyArg
       if (r.id == 0) {
         slots.out[0] = alpha;
         slots.out[1] = beta;
+        slots.out[2] = own;
       }
       __syncthreads();
       alpha = slots.out[0];
       beta = slots.out[1];
+      own = slots.out[2];
     }
     r.store(row, out, [&](float x) {
       const float d = (x - m) * c;
       return fast_exp2(d) * fmaf(beta, fmaxf(d, kLeast), alpha);
     });
-    team_barrier<W>();  // the token's own element comes after its vector
-    if (r.id == 0) put_elem<DT>(out, y, own);
+    // The token's own element comes after its vector, from the same thread.
+    if (r.id == r.owner_of(y)) put_elem<DT>(out, y, own);
   }
 }
 
@@ -567,7 +569,7 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
 // us; sixteen waves, one row to a unit, 280; held whole in sixteen waves'
 // registers, where every unit computes at the same time, 382); sixteen where
 // there are too few rows for that (512 rows of 151936 fp32 logits: 139 us, 145;
-// 24 rows of 32000 bf16: @@).
+// 24 rows of 32000 bf16: 13.9 us with four, 12.4).
 template <int DT>
 int waves_of(const LogitArgs& l) {
   const int vectors = cdiv(l.vocab, Elem<DT>::kPerVec);

@@ -69,21 +69,16 @@ __device__ inline u32x4_any pack(const float (&x)[Elem<DT>::kPerVec]) {
   return v;
 }
 
-// Vector `vec` of a row: elements vec * E .. vec * E + E - 1, all of them in the row.
-template <int DT>
+// Vector `vec` of a row, all of whose elements are in the row.
 __device__ inline u32x4_any load_whole(const void* row, int vec) {
   return *reinterpret_cast<const u32x4_any*>(static_cast<const char*>(row) + (size_t)vec * 16);
-}
-template <int DT>
-__device__ inline void store_whole(void* row, int vec, const float (&x)[Elem<DT>::kPerVec]) {
-  *reinterpret_cast<u32x4_any*>(static_cast<char*>(row) + (size_t)vec * 16) = pack<DT>(x);
 }
 // The same where the row may end inside: elements from `vocab` on are -inf.
 template <int DT>
 __device__ inline u32x4_any load_vec(const void* row, int vec, int vocab) {
   constexpr int E = Elem<DT>::kPerVec;
   const int first = vec * E;
-  if (first + E <= vocab) return load_whole<DT>(row, vec);
+  if (first + E <= vocab) return load_whole(row, vec);
   float x[E];
 #pragma unroll
   for (int k = 0; k < E; ++k) x[k] = first + k < vocab ? Elem<DT>::get(row, first + k) : -INFINITY;

@@ -468,7 +468,7 @@ __device__ inline bool gather(Lds<NT>& l, const Row<DT, NT>& r, uint32_t tau, do
 
 // SPLIT: scan_kernel has been over the row.
 template <int DT, int NT, bool SPLIT>
-__global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(const SampleArgs a) {
   __shared__ Lds<NT> l;
   typedef Key<DT> K;
   constexpr int E = Elem<DT>::kPerVec, kWaves = Lds<NT>::kWaves;
@@ -746,7 +746,6 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       u64 above;
       const u64 slack = by_mass ? (u64)(Z * scale * (V * 0x1p-32 + off)) : 0;  // half a step a token, and Z's
       const int hi = find_top<NT, BINS>(l, from > slack ? from - slack : 1, above, value);
-      const u64 above_count = above;  // where it is the number of tokens
       __syncthreads();
       const int lo = by_mass ? find_top<NT, BINS>(l, to + slack, above, value) : hi;
       if (lo <= 0) return false;
@@ -756,9 +755,12 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
         settled = true;
         return false;
       }
-      const float edge = r.max - (float)(BINS - lo) / per;
+      // Those steps as logits, with room for roundings: what lies there is listed.
+      const auto room = [&](float edge) { return fabsf(edge) * 1e-5f + fit * 1e-5f; };
+      const float first = r.max - (float)(BINS - lo) / per, last = r.max - (float)(BINS - 1 - hi) / per;
+      const float x_lo = first - room(first), x_hi = last + room(last);
       // Z is summed on the way, over every vector.
-      const uint32_t edge_upper = by_mass ? 0 : max(upper, K::upper(K::of(edge - (fabsf(edge) * 1e-5f + fit * 1e-4f))));
+      const uint32_t edge_upper = by_mass ? 0 : max(upper, K::upper(K::of(x_lo)));
       __syncthreads();
       if (tid == 0) {
         l.count = 0;
@@ -766,17 +768,19 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
         l.most = 0;
       }
       __syncthreads();
-      double s = 0.0, others = 0.0;
+      double s = 0.0, every = 0.0;
+      int n_over = 0;
       r.template each<4>(l, edge_upper, [&](int v, const float (&x)[E]) {
         uint32_t in = 0;
         double w[E];
         weights(x, r.max, r.c, w);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const int at = x[e] > -INFINITY ? step(x[e]) : 0;
-          s += at > hi ? w[e] : 0.0;
-          others += at > hi ? 0.0 : w[e];
-          in |= at >= lo && at <= hi ? 1u << e : 0u;
+          const bool over = x[e] > x_hi;
+          s += over ? w[e] : 0.0;
+          every += w[e];
+          n_over += over ? 1 : 0;
+          in |= x[e] >= x_lo && !over ? 1u << e : 0u;
         }
         for (; in != 0; in &= in - 1) {
           const int i = v * E + __builtin_ctz(in), place = atomicAdd(&l.count, 1);
@@ -796,8 +800,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       for (int w = 0; w < kWaves; ++w) over += l.d[w];
       u64 need = from;
       if (by_mass) {
-        double* sums = reinterpret_cast<double*>(l.q);
-        Z = over + block_sum<NT>(others, sums);
+        Z = block_sum<NT>(every, reinterpret_cast<double*>(l.q));
         whole_sum = true;
         need = (u64)fmax(ceil(p * Z * scale), 1.0);
       }
@@ -805,7 +808,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       u64 sum = 0;
       from_list([&](uint32_t, uint32_t, u64 mass) { sum += by_mass ? mass : 1; });
       sum = block_sum<NT>(sum, l.q);
-      const u64 so_far = by_mass ? (u64)(over * scale) : above_count;
+      const u64 so_far = by_mass ? (u64)(over * scale) : (u64)block_sum<NT>(n_over, l.i);
       if (so_far >= need || so_far + sum < need) return false;
       const Cut found = descend(l, l.least, l.most, need - so_far, [&](auto&& f) {
         from_list([&](uint32_t key, uint32_t, u64 mass) { f(key, by_mass ? mass : 1ull); });
@@ -1081,8 +1084,14 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   if (spare_v >= 0 && l.spare == spare_v) finish(walk(spare_v, spare_s, spare_t, INFINITY), total);
 }
 
-// Whether rows are scanned by several workgroups.
-bool sample_splits(int rows, int vocab, int per_vec) { return rows <= 64 && cdiv(vocab, per_vec) > 4096; }
+// Whether rows are scanned by workgroups of their own: where the second launch costs
+// less than the units that one workgroup a row leaves idle (all tokens kept of 1, 64,
+// 128, 192 rows of 128000 bf16 logits: 39, 39, 40, 40 us with a workgroup each, 21, 28,
+// 37, 45 split; of 1, 64, 128 rows of 40000: 20, 21, 22 us, 20, 22, 27 split).
+bool sample_splits(int rows, int vocab, int per_vec) {
+  const int vectors = cdiv(vocab, per_vec);
+  return vectors > 6144 && rows <= vectors / 112;
+}
 
 template <int DT>
 void launch(const SampleArgs& a, hipStream_t stream) {
@@ -1091,13 +1100,21 @@ void launch(const SampleArgs& a, hipStream_t stream) {
   if (sample_splits(a.logits.rows, a.logits.vocab, Elem<DT>::kPerVec)) {
     scan_kernel<DT><<<dim3(a.logits.rows * kSplit), dim3(kScanThreads), 0, stream>>>(a);
     sample_kernel<DT, kSplitThreads, true><<<grid, dim3(kSplitThreads), 0, stream>>>(a);
-  } else if (vectors <= 1024 || (vectors <= 4096 && a.logits.rows > a.logits.num_cus)) {
-    sample_kernel<DT, 256, false><<<grid, dim3(256), 0, stream>>>(a);
-  } else if (vectors <= 16384 && a.logits.rows > a.logits.num_cus) {
-    sample_kernel<DT, 512, false><<<grid, dim3(512), 0, stream>>>(a);
-  } else {
-    sample_kernel<DT, 1024, false><<<grid, dim3(1024), 0, stream>>>(a);
+    return;
   }
+  // Most of a short row's time goes to reductions and barriers, fewer with fewer waves,
+  // and four workgroups to a unit fill each other's waits; longer rows want more loads
+  // and weights at once. Mixed filters, bf16, 256 / 512 / 1024 threads, in us:
+  //   600 x 2000: 21, 27, 49; 300 x 8000: 22, 20, 32; 2000 x 8000: 45, 62, 124;
+  //   256 x 32000: 34, 26, 30; 1000 x 32000: 55, 51, 78; 2000 x 32000: 74, 85, 152;
+  //   512 x 64000: -, 63, 73; 256 x 151936: -, 107, 100; 1024 x 151936: 263, 157, 202.
+  const int rows = a.logits.rows, cus = a.logits.num_cus;
+  if (vectors <= 512 || (vectors <= 4096 && rows > (vectors <= 2048 ? 2 : 4) * cus))
+    sample_kernel<DT, 256, false><<<grid, dim3(256), 0, stream>>>(a);
+  else if (vectors <= 10240 || rows > cus)
+    sample_kernel<DT, 512, false><<<grid, dim3(512), 0, stream>>>(a);
+  else
+    sample_kernel<DT, 1024, false><<<grid, dim3(1024), 0, stream>>>(a);
 }
 
 }  // namespace
