@@ -561,10 +561,11 @@ def distill_loss(logits, ids, values, losses, dlogits=None, *, kind="tail", weig
         raise ValueError(f"kind {kind!r}, not one of {', '.join(RP_DISTILL_KINDS)}")
     device, f32 = _device(), torch.float32
     l = _logits(logits, device)
-    _tensors(("ids", ids, torch.int32, (l.num_rows, None)), ("values", values, f32, (l.num_rows, ids.shape[1])))
+    k = ids.shape[1] if ids.dim() == 2 else 0
+    _tensors(("ids", ids, torch.int32, (l.num_rows, None)), ("values", values, f32, (l.num_rows, k)))
     _per_row(l.num_rows, device, ("losses", losses, f32), ("weights", weights, f32))
     stride = _rows("dlogits", dlogits, device, logits)[2] if dlogits is not None else 0
-    teacher = RpTeacher(_ptr(ids), _ptr(values), ids.shape[1], RP_DISTILL_KINDS[kind], _ptr(weights),
+    teacher = RpTeacher(_ptr(ids), _ptr(values), k, RP_DISTILL_KINDS[kind], _ptr(weights),
                         float(temperature))
     _check(load().rp_distill_loss(ctypes.byref(l), ctypes.byref(teacher), _ptr(losses), _ptr(dlogits), stride,
                                   _work_ptr(workspace, device), _ws_bytes(workspace), _stream(stream)),

@@ -16,8 +16,16 @@
 // passes load only vectors that hold a token they look for. Few tokens above a
 // threshold (all that top-k, or a nucleus of usual size, can keep) become a
 // list in LDS, and the cut and the token are found there by histograms over
-// slices of the keys, and of the indices. Longer lists are found the same way
-// from the row itself.
+// slices of the keys, and of the indices. Where what is kept is more than a list
+// holds, a histogram of the whole row says between which two logits the cut lies,
+// and one pass sums what is above them and lists what is between them.
+//
+// What bounds it (256 rows of 151936 bf16 logits, 11 us to read): without filters
+// 50 us, about 38 of them 64-bit weights (13 instructions a logit, 4 cycles each for
+// a wave); top-k 35 and min-p 29 us, the first pass 23 (32-bit weights) and the rest
+// the chain of short steps between barriers; a nucleus of 10^5 tokens 110 us, the
+// row's two further passes, one of them in 64-bit weights. A single row takes 15 to
+// 25 us, nearly all in that chain.
 #include "rp_rows.h"
 
 namespace rp {
@@ -715,10 +723,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
     };
     // Where the tokens that are kept are many: their number, or their weight in steps
     // of 2^-31 of the row's, by equal steps of the logits says which of those the cut
-    // lies in; then
-    // one pass sums what is above those steps, by stretch, and lists what is in them.
-    // Tokens at `least` and below do not count: LDS would add to one bin for most of
-    // a wave. False where that does not settle it.
+    // lies in; then one pass sums what is above those steps, by stretch, and lists what
+    // is in them. Tokens at `least` and below do not count: LDS would add to one bin
+    // for most of a wave. False where that does not settle it. (512 flat rows of 50257
+    // fp32 logits: 89 us; three passes with 64-bit masses in the bins, from_row, 186.)
     bool settled = false;  // cut and ties are known
     bool whole_sum = false;  // Z is the sum in 64 bits
     const auto wide = [&](bool by_mass, u64 from, u64 to, float low, uint32_t upper, float least) __attribute__((always_inline)) {

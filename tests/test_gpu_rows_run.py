@@ -180,6 +180,8 @@ def test_tensors_that_are_refused():
         rp.policy_loss(x, i, f, f[:2], f)
     with pytest.raises(ValueError, match="values"):
         rp.distill_loss(x, torch.zeros(n, 3, dtype=torch.int32, device="cuda"), torch.zeros(n, 2, device="cuda"), f)
+    with pytest.raises(ValueError, match="ids"):
+        rp.distill_loss(x, i, f, f)
     wide = torch.zeros(2, 1 << 20, device="cuda")
     with pytest.raises(rp.RpError) as e:
         rp.sample_tokens(wide, f[:2], i[:2])
