@@ -518,7 +518,7 @@ typedef struct {
 /* Draw a token from every row: with W the weights' sum over the kept tokens,
  * the least index i such that the weights of the kept tokens 0 .. i sum to
  * more than u[n] W (u: fp32 [num_rows], in [0, 1); values outside are taken
- * for the nearest inside, NaN for 0). Weights and their sums are held in 64
+ * for the nearest inside, NaN for 0; a token of weight 0 is never drawn). Weights and their sums are held in 64
  * bits: the token is that of exact arithmetic unless u W lies within about
  * 1e-12 W of a border (a step of u is 6e-8).
  * tokens: int32 [num_rows]. logprobs (fp32 [num_rows], or NULL): ln of the
@@ -546,7 +546,9 @@ rp_status rp_token_logprobs(const rp_logits* logits, const int32_t* tokens, doub
  * Rows whose token is outside [0, vocab), or whose row_seq is outside
  * [0, num_advantages), are skipped: their logits are not read, and loss,
  * log-probability, entropy and gradient are 0. A weight of 0 gives loss and
- * gradient 0 whatever else the row holds. */
+ * gradient 0 whatever else the row holds. A token whose own logit is -inf has
+ * l = -inf and r = 0; there k has no finite value, and with kl_beta the loss is
+ * not a number and the gradient not finite. */
 typedef struct {
   const int32_t* tokens;        /* [num_rows] */
   const float* old_logprobs;    /* [num_rows], of the policy that drew the tokens */
@@ -573,8 +575,9 @@ rp_status rp_policy_loss(const rp_logits* logits, const rp_policy_batch* batch,
 
 /* Distillation from a teacher that gives its likeliest tokens only: row n
  * lists ids[n][j] with values[n][j], j < k. Entries outside [0, vocab), entries
- * whose value is -inf, and ids that the row lists before do not count. With q
- * the student's probabilities at `temperature`, over the entries that count:
+ * whose value is -inf, and entries with the id of an earlier one that counts do
+ * not count. With q the student's probabilities at `temperature`, over the
+ * entries that count:
  *   RP_DISTILL_TOPK: values are the teacher's logits (or log-probabilities),
  *     P = softmax(values / temperature) over the list, loss = sum P (ln P - ln q).
  *   RP_DISTILL_TAIL: values are log-probabilities at `temperature`, P =
