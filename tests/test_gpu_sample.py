@@ -72,6 +72,19 @@ def test_sampling(n, V, dtype, pad, offset, masked, filters):
     assert gaps_untouched(view, buf)
 
 
+@pytest.mark.parametrize("scale", [0.5, 2.5])
+@pytest.mark.parametrize("n,V,dtype", [(90, 90001, "bf16"), (170, 90001, "f16"), (270, 40001, "f32"), (520, 9001, "bf16")])
+def test_batches_that_fill_the_units(n, V, dtype, scale):
+    """Rows scanned apart above 64 of them, and a workgroup of each size to a row; flat rows and rows with peaks."""
+    say(f"batch {n} x {V} {dtype} scale {scale}")
+    rng = np.random.default_rng(n)
+    x, view, buf = logits(rng, n, V, dtype, scale=scale, peaks=4 if scale > 1 else 0)
+    u = rng.random(n).astype(np.float32)
+    for filters in ("none", "topp", "all"):
+        _check(x, view, u, _params(rng, n, filters), filters)
+    assert gaps_untouched(view, buf)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("filters", ["topk", "topp", "minp", "all"])
 def test_many_equal_logits(dtype, filters):
