@@ -87,7 +87,9 @@ __device__ inline u32x4_any load_vec(const void* row, int vec, int vocab) {
 
 // Sums and maxima over a wave and over a workgroup of NT threads, in every
 // thread; `lds` has a slot per wave. The workgroup forms begin with a barrier,
-// so the slots may be used again at once. The order of additions is fixed.
+// so one may follow another on the same slots at once; they end with reads of
+// them, so whatever else writes there needs a barrier first. The order of
+// additions is fixed.
 template <class T>
 __device__ inline T wave_sum(T x) {
 #pragma unroll

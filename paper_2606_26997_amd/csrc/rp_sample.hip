@@ -355,9 +355,15 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(const SampleArgs a) 
 }
 
 // The place, from the top of BINS bins, where the sums of value(bin) reach `need`
-// (at most all of it): its bin, and the sum above.
+// (at most all of it): its bin, the sum above, and that of all bins. A barrier has to
+// lie between whatever last read l.q, l.bin or l.above and this, which writes them
+// before its own first one.
+struct Place {
+  int bin;
+  u64 above, all;
+};
 template <int NT, int BINS, class Value>
-__device__ inline int find_top(Lds<NT>& l, u64 need, u64& above, const Value& value) {
+__device__ inline Place find_top(Lds<NT>& l, u64 need, const Value& value) {
   constexpr int PER = BINS / NT;
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   u64 h[PER], sum = 0;
@@ -394,13 +400,12 @@ __device__ inline int find_top(Lds<NT>& l, u64 need, u64& above, const Value& va
     }
   }
   __syncthreads();
-  above = l.above;
-  return l.bin;
+  return {l.bin, l.above, all};
 }
 
 template <int NT>
-__device__ inline int find_top(Lds<NT>& l, u64 need, u64& above) {
-  return find_top<NT, kBins>(l, need, above, [&](int bin) { return l.hist[bin]; });
+__device__ inline Place find_top(Lds<NT>& l, u64 need) {
+  return find_top<NT, kBins>(l, need, [&](int bin) { return l.hist[bin]; });
 }
 
 template <int NT>
@@ -428,10 +433,10 @@ __device__ __attribute__((always_inline)) inline Cut descend(Lds<NT>& l, uint32_
       if (key - lo <= width) atomicAdd(&l.hist[(key - lo) >> s], mass);
     });
     __syncthreads();
-    u64 above;
-    const uint32_t bin = (uint32_t)find_top(l, need, above);
-    need -= above < need ? above : need;
-    over += above;
+    const Place at = find_top(l, need);
+    const uint32_t bin = (uint32_t)at.bin;
+    need -= at.above < need ? at.above : need;
+    over += at.above;
     lo += bin << s;
     if (s == 0) return {lo, over};
     width = min(width - (bin << s), (1u << s) - 1);
@@ -563,10 +568,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
       if (tid == 0) l.least = 0xFFFFFFFFu;
       __syncthreads();
       if (has) atomicAdd(&l.hist[bin], mine);
-      if (block_sum<NT>(mine, l.q) < need) return 0u;
-      u64 above;
-      const int at = find_top(l, need, above);
-      if (has && bin >= at) atomicMin(&l.least, K::of(top));
+      __syncthreads();
+      const Place at = find_top(l, need);
+      if (at.all < need) return 0u;
+      if (has && bin >= at.bin) atomicMin(&l.least, K::of(top));
       __syncthreads();
       return l.least;
     };
@@ -679,9 +684,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
           if (x[e] > -INFINITY) atomicAdd(&l.hist[step(x[e])], one(x[e]));
       });
       __syncthreads();
-      u64 above;
-      const int at = find_top(l, need, above);
-      need -= above < need ? above : need;
+      const Place place = find_top(l, need);
+      const int at = place.bin;
+      need -= place.above < need ? place.above : need;
       // The keys of that step, and a threshold for the vectors that hold them.
       const float edge = at == 0 ? -INFINITY : r.max - (float)(kBins - at) / per;
       const float slack = at == 0 ? 0.f : fabsf(edge) * 1e-5f + fit * 1e-4f;
@@ -709,7 +714,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
           }
         });
       });
-      found.above += above;
+      found.above += place.above;
       return found;
     };
 
@@ -751,11 +756,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
       const auto value = [&](int bin) __attribute__((always_inline)) {
         return by_mass ? (u64)((double)counts[bin] * (0x1p-31 * Z * scale)) : (u64)counts[bin];
       };
-      u64 above;
       const u64 slack = by_mass ? (u64)(Z * scale * (V * 0x1p-32 + off)) : 0;  // half a step a token, and Z's
-      const int hi = find_top<NT, BINS>(l, from > slack ? from - slack : 1, above, value);
+      const int hi = find_top<NT, BINS>(l, from > slack ? from - slack : 1, value).bin;
       __syncthreads();
-      const int lo = by_mass ? find_top<NT, BINS>(l, to + slack, above, value) : hi;
+      const int lo = by_mass ? find_top<NT, BINS>(l, to + slack, value).bin : hi;
       if (lo <= 0) return false;
       if (key_q > 0 && step(K::logit(key_q)) > hi) {
         cut = key_q;
