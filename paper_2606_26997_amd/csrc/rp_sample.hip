@@ -34,6 +34,9 @@ namespace {
 typedef unsigned long long u64;
 constexpr int kBins = 1024;
 constexpr int kNoCrossing = 0x7FFFFFFF;
+// A stretch whose kept weight is less adds nothing. Above it, some token there has a
+// weight of its own above 0, whichever way the sum was taken.
+constexpr double kLeastSum = 0x1p-1000;
 
 // A listed token: its place in the order of keys, then of falling indices, and its weight.
 struct Token {
@@ -994,8 +997,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
   }
   __syncthreads();
   // Every wave finds the stretch, its lanes w < kWaves holding the sums up to stretch w.
-  double upto_w = lane < kWaves ? l.d[lane] : 0.0;
-  int ties_w = lane < kWaves ? l.i[lane] : 0;
+  const double own_w = lane < kWaves ? l.d[lane] : 0.0;
+  const int own_t = lane < kWaves ? l.i[lane] : 0;
+  double upto_w = own_w;
+  int ties_w = own_t;
 #pragma unroll
   for (int o = 1; o < kWaves; o <<= 1) {
     const double us = __shfl_up(upto_w, o);
@@ -1006,27 +1011,32 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
     }
   }
   const double total = held(__shfl(upto_w, kWaves - 1), __shfl(ties_w, kWaves - 1)), target = part * total;
-  const u64 crossed = __ballot(lane < kWaves && held(upto_w, ties_w) > target) | 1ull << (kWaves - 1);
-  const int where = __builtin_ctzll(crossed);
+  // Running sums that are added in different orders differ by roundings, also between two
+  // neighbours of which the second keeps nothing. So the border is looked for where
+  // something is added (here, and among vectors and tokens below), and lies in the last
+  // of those where no sum passes the target.
+  const bool adds_w = own_w > kLeastSum || (own_t > 0 && ties_w - own_t < ties && w_cut > 0.0);
+  const u64 adding = __ballot(adds_w), crossed = __ballot(adds_w && held(upto_w, ties_w) > target);
+  const int where = crossed != 0 ? __builtin_ctzll(crossed) : 63 - __builtin_clzll(adding);
   double before = where > 0 ? __shfl(upto_w, max(where - 1, 0)) : 0.0;
   int tie_before = where > 0 ? __shfl(ties_w, max(where - 1, 0)) : 0;
-  // Sums in another order may miss the crossing by a rounding; then it is the stretch's last kept token.
   const int base = where * r.steps * 64, vectors = r.steps * 64;
   int spare_v = -1, spare_t = 0;
   double spare_s = 0.0;
-  // The first token of a vector that passes the limit, or its last kept one.
+  // The first kept token of a vector that passes the limit, or its last one.
   const auto walk = [&](int v, double ms, int mt, double limit) __attribute__((always_inline)) {
     float x[E];
     unpack<DT>(load_vec<DT>(r.data, v, V), x);
     int found = -1, last = -1;
-    double at = held(ms, mt);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      add(x[e], ms, mt);
-      const double now = held(ms, mt);
-      if (now > limit && found < 0) found = v * E + e;
-      if (now > at) last = v * E + e;
-      at = now;
+      double own = 0.0;
+      const int before_t = mt;
+      add(x[e], own, mt);
+      ms += own;
+      if (!(own > 0.0 || (mt > before_t && before_t < ties && w_cut > 0.0))) continue;
+      last = v * E + e;
+      if (held(ms, mt) > limit && found < 0) found = last;
     }
     return found >= 0 ? found : last;
   };
@@ -1076,12 +1086,13 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
     }
     const double from = upto - s;
     const int from_t = upto_t - t;
-    if (held(from + s, upto_t) > held(from, from_t)) {
+    const bool adds = s > 0.0 || (t > 0 && from_t < ties && w_cut > 0.0);
+    if (adds) {
       spare_v = v;
       spare_s = from;
       spare_t = from_t;
     }
-    const bool over = held(upto, upto_t) > target;
+    const bool over = adds && held(upto, upto_t) > target;
     if (over) atomicMin(&l.first, v);
     __syncthreads();
     if (l.first != kNoCrossing) {

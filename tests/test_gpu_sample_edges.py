@@ -1,4 +1,8 @@
-"""Sampling on the GPU where its forms could part from the definition: many rows that draw alike."""
+"""Sampling on the GPU where its forms could part from the definition: many rows that draw alike, borders
+between sums that differ by a rounding."""
+import math
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -37,3 +41,107 @@ def test_rows_alike_draw_alike(n, V, dtype):
             tokens, lp, kept = _draw(view, np.repeat(u, n), **alike)
             assert (tokens == int(want[0])).all(), how
             assert (lp == lp[0]).all() and (kept == kept[0]).all(), how
+
+
+def _weight(x):
+    """2^(x log2 e) by the kernel's polynomial, products and sums rounded once together."""
+    y = max(x * 1.4426950408889634, -1500.0)
+    n = round(y)
+    f = Fraction(y) - n
+    p = 0.0
+    for c in ("0x1.b63881021ff95p-24", "0x1.63d13637e6ed6p-20", "0x1.ffcb95154c637p-17", "0x1.4308ac85a8c94p-13",
+              "0x1.5d87fe86fea1bp-10", "0x1.3b2ab7181b769p-7", "0x1.c6b08d7047e52p-5", "0x1.ebfbdff823cedp-3",
+              "0x1.62e42fefa39efp-1", "0x1p0"):
+        p = float(Fraction(p) * f + Fraction(float.fromhex(c)))
+    return math.ldexp(p, n)
+
+
+def _butterfly(s):
+    """A wave's sum [..][64], lane by lane."""
+    for o in (32, 16, 8, 4, 2, 1):
+        s = s + s[..., np.arange(64) ^ o]
+    return s[..., 0]
+
+
+def _scan(s):
+    """Running sums over the lanes, by doubling."""
+    for o in (1, 2, 4, 8, 16, 32):
+        if o < s.shape[-1]:
+            s = np.concatenate([s[..., :o], s[..., o:] + s[..., :-o]], -1)
+    return s
+
+
+def _vector_sums(w):
+    s = np.zeros(w.shape[:-1])
+    for e in range(w.shape[-1]):
+        s = s + w[..., e]
+    return s
+
+
+def _vectors(rng, count):
+    """Logits in steps of 1/32 that bf16 holds, 0 the largest of every vector."""
+    x = -rng.integers(1, 97, (count, 8)) / 32.0
+    x[:, 0] = 0.0
+    return x
+
+
+def _gap_in_a_wave(rng, w_of):
+    """Rows of two stretches of 64 vectors; behind the first one's last kept vector the scan's sums differ by a rounding,
+    and half of the row's weight lies between them."""
+    rows = []
+    while len(rows) < 16:
+        live = int(rng.integers(5, 40))
+        at = np.sort(rng.permutation(60)[:live])
+        x = np.full((128, 8), -np.inf)
+        x[at] = _vectors(rng, live)
+        sums = _vector_sums(w_of(x[:64]))
+        upto, D0 = _scan(sums), _butterfly(sums)
+        least, most = upto[at[-1]], upto[at[-1] + 1:].max()
+        if not (D0 > least and most > least):
+            continue
+        for _ in range(200):
+            x[64:] = -np.inf
+            x[64 + rng.permutation(64)[:live]] = x[at][rng.permutation(live)]
+            target = 0.5 * (D0 + _butterfly(_vector_sums(w_of(x[64:]))))
+            over = np.flatnonzero(upto > target)
+            if D0 > target and over.size and over[0] > at[-1]:
+                rows.append(x.reshape(-1).copy())
+                break
+    return np.array(rows)
+
+
+def _gap_between_stretches(rng, w_of):
+    """Rows of eight stretches of 128 vectors, the fourth masked, whose running sum is a rounding above the third's; half of
+    the row's weight lies between them."""
+    rows = []
+    while len(rows) < 16:
+        x = np.full((8, 2, 64, 8), -np.inf)
+        x[:3] = _vectors(rng, 3 * 128).reshape(3, 2, 64, 8)
+        for _ in range(50):
+            x[4:7] = x[:3].reshape(-1, 8)[rng.permutation(3 * 128)].reshape(3, 2, 64, 8)
+            D = _vector_sums(w_of(x))
+            D = _butterfly(D[:, 0] + D[:, 1])
+            upto = _scan(D)
+            target = 0.5 * upto[-1]
+            if np.flatnonzero(upto > target)[0] == 3:
+                rows.append(x.reshape(-1).copy())
+                break
+    return np.array(rows)
+
+
+@pytest.mark.parametrize("rows_of", [_gap_in_a_wave, _gap_between_stretches])
+def test_a_border_between_two_roundings(rows_of):
+    """Running sums that were added in different orders may differ by a rounding from one masked token to the next; a
+    border that falls between two such sums still draws a token that can occur."""
+    say(f"borders: {rows_of.__name__}")
+    table = np.array([_weight(-i / 32.0) for i in range(97)] + [0.0])
+    w_of = lambda x: table[np.where(np.isfinite(x), -32 * np.maximum(x, -3.0), 97).astype(int)]
+    x = rows_of(np.random.default_rng(17), w_of)
+    view = torch.from_numpy(x).to("cuda", torch.bfloat16)
+    tokens = _draw(view, np.full(len(x), 0.5))[0].tolist()
+    assert all(0 <= t < x.shape[1] and r[t] > -np.inf for t, r in zip(tokens, x)), tokens
+    # It is one of the two beside the border: exact arithmetic does not tell which.
+    for t, r in zip(tokens, x):
+        w = np.exp(r)
+        before, upto = w[:t].sum() / w.sum(), w[:t + 1].sum() / w.sum()
+        assert before - 1e-12 <= 0.5 <= upto + 1e-12
