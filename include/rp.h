@@ -503,7 +503,8 @@ rp_status rp_logits_workspace_size(const rp_logits* logits, size_t* bytes);
  * The vocabulary is sorted by logit, the lowest index first among equals; the
  * tokens kept are the first min(n_k, n_p, n_m), at least one:
  *   temperature T (NULL: 1): weights w_i = exp((x_i - max x) / T). T <= 0 (or
- *     NaN) is greedy: the largest logit of the lowest index is taken.
+ *     NaN) is greedy: the largest logit of the lowest index is taken. T = +inf
+ *     weighs all tokens that can occur alike.
  *   top_k (NULL or <= 0: all): n_k = min(top_k, vocab).
  *   top_p (NULL, NaN or >= 1: all): n_p is the least n with
  *     w_1 + .. + w_n >= top_p (w_1 + .. + w_{n_k}).

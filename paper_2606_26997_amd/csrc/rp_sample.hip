@@ -202,13 +202,16 @@ struct Row {
   }
 };
 
-// How row n is sampled. Greedy is top-1 at T = 1. c stays above 0, so that -inf
-// weighs nothing at T = inf too.
+// How row n is sampled. Greedy is top-1 at T = 1. c = log2(e) / T stays above 0, so
+// that -inf weighs nothing at T = inf too, in 64 bits. In 32 bits c would be 0 there,
+// and where T is far from 1 it loses digits, or a difference of logits that still
+// counts passes fp32's largest number (odd): such rows are done in 64 bits throughout.
 struct How {
   int k;        // vocab: all
   double p, q;  // 1 and 0: all
-  double inv_t;
+  double inv_t, c;
   bool all, light;  // all: a border hangs on every token's weight; light: k few enough for a list
+  bool odd, exact;  // exact: the row's sum is in 64 bits
   __device__ inline How(const SampleArgs& a, int n, int lightest) {
     const int V = a.logits.vocab;
     const float T = a.temperature != nullptr ? a.temperature[n] : 1.f;
@@ -218,10 +221,13 @@ struct How {
     const float asked_q = greedy || a.min_p == nullptr ? 0.f : a.min_p[n];
     k = asked_k > 0 && asked_k < V ? asked_k : V;
     p = asked_p < 1.f ? fmax((double)asked_p, 0.0) : 1.0;
-    q = asked_q > 0.f ? fmin((double)asked_q, 1.0) : 0.0;
+    q = asked_q > 0.f && T < INFINITY ? fmin((double)asked_q, 1.0) : 0.0;  // at T = inf all weigh 1
     inv_t = greedy ? 1.0 : fmax(1.0 / (double)T, 1e-300);
+    c = kLog2e64 * inv_t;
+    odd = !(c >= 1e-30 && c <= 1e38);
     light = k < V && k <= lightest;
     all = k >= V && p >= 1.0 && q == 0.0;
+    exact = all || odd;
   }
 };
 
@@ -242,7 +248,7 @@ __device__ __attribute__((always_inline)) inline Scan scan(const Row<DT, NT>& r,
   constexpr int E = Elem<DT>::kPerVec, U = 4;
   typedef Key<DT> K;
   Scan o;
-  const float c32 = (float)fmin(r.c, 3e38);
+  const float c32 = (float)r.c;
   const int each = (1 << r.shift) - 1, count = r.entries > first ? cdiv(r.entries - first, stride) << r.shift : 0;
   const auto at = [&](int i) { return ((i >> r.shift) * stride + first) << r.shift | (i & each); };
   u32x4_any next[U];
@@ -313,7 +319,7 @@ template <int DT, int NT>
 __device__ inline double sum_to(const Scan& o, const Row<DT, NT>& r, float max, bool exact) {
   if (!(o.ref > -INFINITY)) return 0.0;
   if (exact) return o.s * weight(o.ref, max, r.c);
-  const float c32 = (float)fmin(r.c, 3e38);
+  const float c32 = (float)r.c;
   if (o.top < max) return (double)((o.rest + o.group) * fast_exp2((o.ref - max) * c32));
   // The vector with the maximum again, in 64 bits: where one token has nearly all
   // the mass, ln Z is that of the rest.
@@ -347,13 +353,13 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(const SampleArgs a) 
   SplitRow& out = static_cast<SplitRow*>(a.workspace)[n];
   Row<DT, kSplitThreads> r(a.logits, n);
   const How how(a, n, kSplitThreads / 2);
-  r.c = kLog2e64 * how.inv_t;
+  r.c = how.c;
   const int thread = stretch * 64 + tid % 64;
-  const Scan o = scan(r, thread, tid / 64, kScanThreads / 64, how.all,
+  const Scan o = scan(r, thread, tid / 64, kScanThreads / 64, how.exact,
                       [&](int g, uint16_t key) { out.top[g * kSplitThreads + thread] = key; });
   const float top = block_max<kScanThreads>(o.top, lds_f);
   const bool bad = __syncthreads_or(o.bad);
-  const double s = block_sum<kScanThreads>(bad ? 0.0 : sum_to(o, r, top, how.all), lds_d);
+  const double s = block_sum<kScanThreads>(bad ? 0.0 : sum_to(o, r, top, how.exact), lds_d);
   if (tid == 0) out.part[stretch] = {top, bad ? 1 : 0, s};
 }
 
@@ -491,7 +497,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
   const int n = blockIdx.x, V = a.logits.vocab, tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
   Row<DT, NT> r(a.logits, n);
   const How how(a, n, NT / 2);
-  r.c = kLog2e64 * how.inv_t;
+  r.c = how.c;
   const int k = how.k;
   const double p = how.p, q = how.q, inv_t = how.inv_t;
   const bool light_k = how.light, all = how.all;
@@ -504,8 +510,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
     r.max = wave_max(part.top);
     bad = __ballot(part.bad != 0) != 0;
     if (tid < kSplit && part.top > -INFINITY)
-      l.d[tid] = part.s * (how.all ? weight(part.top, r.max, r.c)
-                                     : (double)fast_exp2((part.top - r.max) * (float)fmin(r.c, 3e38)));
+      l.d[tid] = part.s * (how.exact ? weight(part.top, r.max, r.c)
+                                     : (double)fast_exp2((part.top - r.max) * (float)r.c));
     else if (tid < kSplit) l.d[tid] = 0.0;
     uint32_t most = 0;
     for (int g = 0; g < r.entries; ++g) {
@@ -516,12 +522,12 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
     const uint32_t o = most << 16;
     if (most > 0x007Fu) top = __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
   } else {
-    const Scan o = scan(r, tid, 0, 1, how.all, [&](int g, uint16_t key) { l.top[g * NT + tid] = key; });
+    const Scan o = scan(r, tid, 0, 1, how.exact, [&](int g, uint16_t key) { l.top[g * NT + tid] = key; });
     top = o.top;
     r.max = block_max<NT>(top, l.f);
     bad = __syncthreads_or(o.bad);
     if (!bad && r.max > -INFINITY) {
-      const double s = wave_sum(sum_to(o, r, r.max, how.all));
+      const double s = wave_sum(sum_to(o, r, r.max, how.exact));
       if (lane == 0) l.d[wave] = s;
     }
   }
@@ -736,11 +742,11 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
     // for most of a wave. False where that does not settle it. (512 flat rows of 50257
     // fp32 logits: 89 us; three passes with 64-bit masses in the bins, from_row, 186.)
     bool settled = false;  // cut and ties are known
-    bool whole_sum = false;  // Z is the sum in 64 bits
+    bool whole_sum = how.odd;  // Z is the sum in 64 bits
     const auto wide = [&](bool by_mass, u64 from, u64 to, float low, uint32_t upper, float least) __attribute__((always_inline)) {
       constexpr int BINS = 2 * kBins;
       uint32_t* counts = reinterpret_cast<uint32_t*>(l.hist);
-      const float c32 = (float)fmin(r.c, 3e38), fine = (float)(0x1p31 / Z);
+      const float c32 = (float)r.c, fine = (float)(0x1p31 / Z);
       const float fit = fmaxf(fminf(r.max - low, 1e30f), 1e-30f), per = (BINS - 2) / fit;
       const auto step = [&](float x) __attribute__((always_inline)) { return BINS - 1 - (int)fminf((r.max - x) * per, BINS - 1.f); };
       __syncthreads();
@@ -877,8 +883,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
     if (probe && !listed) {
       cut = K::kNegInf;
       ties = 0;
-      summed = wide(true, need_lo, need_hi, low, low_upper, sure ? low - low_slack : -INFINITY);
-    } else if (!listed && k < V && p >= 1.0 && tokens_at_all() > k) {
+      summed = !how.odd && wide(true, need_lo, need_hi, low, low_upper, sure ? low - low_slack : -INFINITY);
+    } else if (!listed && !how.odd && k < V && p >= 1.0 && tokens_at_all() > k) {
       summed = wide(false, (u64)k, (u64)k, r.max - 2.f * (r.max - least_top), 0, -INFINITY);
     }
 

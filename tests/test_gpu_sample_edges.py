@@ -1,5 +1,5 @@
 """Sampling on the GPU where its forms could part from the definition: many rows that draw alike, borders
-between sums that differ by a rounding."""
+between sums that differ by a rounding, temperatures far from 1."""
 import math
 from fractions import Fraction
 
@@ -9,6 +9,7 @@ import torch
 
 import oracle
 from tests.rows_util import dev, empty, logits, say, workspace
+from tests.test_gpu_sample import _check
 
 pytestmark = pytest.mark.gpu
 
@@ -145,3 +146,36 @@ def test_a_border_between_two_roundings(rows_of):
         w = np.exp(r)
         before, upto = w[:t].sum() / w.sum(), w[:t + 1].sum() / w.sum()
         assert before - 1e-12 <= 0.5 <= upto + 1e-12
+
+
+@pytest.mark.parametrize("masked", [0, 3])
+@pytest.mark.parametrize("n,V,dtype", [(10, 9, "f16"), (10, 9000, "bf16"), (10, 70001, "f16"), (10, 60000, "f32")])
+def test_temperatures_without_a_bound(n, V, dtype, masked):
+    """T = +inf makes every token that can occur equally likely, whatever is filtered; temperatures at both ends of fp32."""
+    say(f"temperature inf {n} x {V} {dtype} masked {masked}")
+    rng = np.random.default_rng(V + masked)
+    x, view, _ = logits(rng, n, V, dtype, masked=masked)
+    live = V - masked
+    # Shares of a vocabulary that are no whole number of tokens.
+    p = ((rng.integers(0, live, n) + 0.5) / live).astype(np.float32)
+    k = np.array([1, 2, 3, 40, 200, 700, live // 2, live - 1, live, V + 1], np.int32)
+    q = np.array([0, 1e-30, 0.1, 0.5, 0.999, 1, 1, 0.3, 2, 0.7], np.float32)
+    half = np.full(n, 0.5 + 0.25 / live, np.float32)
+    for T in (np.full(n, np.inf, np.float32), np.array([np.inf, 1e30, 3e38, 1e38, 2e30, 1e-39, 1e-45, 1e-30, 1e10, np.inf], np.float32)):
+        u = rng.random(n).astype(np.float32)
+        for how in (dict(top_k=k), dict(top_p=p), dict(min_p=q), dict(top_k=k, top_p=half), dict(top_k=k, min_p=q),
+                    dict(top_p=p, min_p=q), dict(top_k=k, top_p=half, min_p=q)):
+            _check(x, view, u, dict(temperature=T, **how), str(list(how)))
+
+
+def test_temperatures_of_rows_at_the_ends_of_fp32():
+    """Logits further apart than fp32's largest number: at T = 1e38 each counts."""
+    say("temperature, logits of +-3e38")
+    n, V = 6, 5000
+    view = torch.linspace(-3.2e38, 3.2e38, V, dtype=torch.float64).float().cuda().repeat(n, 1)
+    x = view.double().cpu().numpy()
+    T = np.array([1e38, 3e38, np.inf, 1e37, 1e36, 2e38], np.float32)
+    u = np.random.default_rng(2).random(n).astype(np.float32)
+    f = lambda v: np.full(n, v, np.float32)
+    for how in (dict(), dict(top_k=np.full(n, 70, np.int32)), dict(top_p=f(0.37)), dict(min_p=f(0.3))):
+        _check(x, view, u, dict(temperature=T, **how), str(list(how)))
