@@ -23,6 +23,14 @@ def log_softmax(x, temperature=1.0):
     return z - math.log(math.fsum(np.exp(z)))
 
 
+def log_sum(logs):
+    """ln of the sum of exp(logs); -inf where none is finite."""
+    if not (logs > -np.inf).any():
+        return -math.inf
+    top = logs.max()
+    return top + math.log(math.fsum(np.exp(logs - top)))
+
+
 def _entropy(lp):
     seen = lp[lp > -np.inf]
     return -math.fsum(np.exp(seen) * seen)
@@ -166,17 +174,19 @@ def distill_loss(x, ids, values, *, kind="tail", weights=None, temperature=1.0):
             rest = max(1 - math.fsum(P), TAIL)
             others = np.ones(V, bool)
             others[at] = False
-            out = math.fsum(q[others])
-            gap = math.log(out / rest) if out > 0 else 0.0
+            # Where the mass outside is below float64's range it still has a logarithm.
+            log_out = log_sum(l[others])
+            outside, out = log_out > -math.inf, math.exp(log_out)
+            gap = log_out - math.log(rest) if outside else 0.0
             if kind == "tail":
-                value = math.fsum(np.where(P > 0, P * (t - lq), 0.0)) - (rest * gap if out > 0 else 0.0)
-                whole = math.fsum(P) + (rest if out > 0 else 0.0)
-                d = q * (whole - rest / out) if out > 0 else np.zeros(V)
+                value = math.fsum(np.where(P > 0, P * (t - lq), 0.0)) - (rest * gap if outside else 0.0)
+                whole = math.fsum(P) + (rest if outside else 0.0)
+                d = whole * q - rest * np.exp(np.where(others, l - log_out, -np.inf)) if outside else np.zeros(V)
                 d[at] = whole * q[at] - P
             else:
                 with np.errstate(invalid="ignore"):
                     value = math.fsum(np.where(q[at] > 0, q[at] * (lq - t), 0.0)) + out * gap
-                    d = q * (gap - value) if out > 0 else np.zeros(V)
+                    d = q * (gap - value) if outside else np.zeros(V)
                     d[at] = np.where(q[at] > 0, q[at] * (lq - t - value), 0.0)
         loss[r], grad[r] = w * value, w / temperature * d
     return loss, grad

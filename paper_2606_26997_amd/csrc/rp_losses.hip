@@ -93,20 +93,26 @@ __device__ inline void join(const Stats& a, float max, float c, double& s, doubl
 // barrier before its next one.
 template <int W>
 struct Slots {
-  float m[W];
+  float m[W][3];
   double d[W][5];
   float out[3];
 };
-template <int W>
-__device__ inline float team_max(float x, Slots<W>& s) {
-  x = wave_max(x);
-  if constexpr (W == 1) return x;
-  if (threadIdx.x % 64 == 0) s.m[threadIdx.x / 64] = x;
-  __syncthreads();
-  x = s.m[0];
+template <int W, int N>
+__device__ inline void team_max(float (&x)[N], Slots<W>& s) {
 #pragma unroll
-  for (int w = 1; w < W; ++w) x = fmaxf(x, s.m[w]);
-  return x;
+  for (int i = 0; i < N; ++i) x[i] = wave_max(x[i]);
+  if constexpr (W == 1) return;
+  if (threadIdx.x % 64 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s.m[threadIdx.x / 64][i] = x[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    x[i] = s.m[0][i];
+#pragma unroll
+    for (int w = 1; w < W; ++w) x[i] = fmaxf(x[i], s.m[w][i]);
+  }
 }
 template <int W, int N>
 __device__ inline void team_sum(double (&x)[N], Slots<W>& s) {
@@ -267,11 +273,13 @@ __device__ inline char* grad_row(void* g, long long stride, int n) {
 }
 
 // The row's maximum, and its sums of e and e d in 64 bits, in every thread. masked(v, x)
-// takes what is not summed out of vector v. Rows whose logits times c come near
-// fp32's end are summed by the other form, (x - max) c.
-template <int W, bool ONCE, class R, class Masked>
+// takes what is not summed, nor looked at for the maximum, out of vector v. tops[0]
+// becomes the maximum (fp32's least number where nothing is summed), other entries
+// their own maxima over the team. Rows whose logits times c come near fp32's end are
+// summed by the other form, (x - max) c.
+template <int W, bool ONCE, int N, class R, class Masked>
 __device__ inline float row_sums(R& r, const char* row, float c, const Masked& masked, Slots<W>& slots, double (&sums)[2],
-                                 float top) {
+                                 float (&tops)[N]) {
   constexpr int E = R::E;
   Stats st;
   r.template each<ONCE>(row, [&](int v, const float (&x)[E]) {
@@ -281,7 +289,9 @@ __device__ inline float row_sums(R& r, const char* row, float c, const Masked& m
     masked(v, y);
     add_values(st, v, y, c);
   });
-  const float m = team_max<W>(fmaxf(st.top, top), slots);
+  tops[0] = st.top;
+  team_max<W>(tops, slots);
+  const float m = tops[0];
   const auto reload = [&](int v, float (&x)[E]) {
     r.again(row, v, x);
     masked(v, x);
@@ -326,7 +336,8 @@ __global__ __launch_bounds__(threads_of<W>()) void logprobs_kernel(const Logprob
   const float c = (float)(a.inv_t * kLog2e64), at = Elem<DT>::get(row, y);
   r.fetch_all(row);
   double sums[2];
-  const float m = row_sums<W, true>(r, row, c, [](int, float (&)[Elem<DT>::kPerVec]) {}, slots, sums, -INFINITY);
+  float tops[1];
+  const float m = row_sums<W, true>(r, row, c, [](int, float (&)[Elem<DT>::kPerVec]) {}, slots, sums, tops);
   team_sum<W>(sums, slots);
   if (r.id == 0) {
     const bool empty = sums[0] == 0.0;
@@ -360,7 +371,8 @@ __global__ __launch_bounds__(threads_of<W>()) void policy_kernel(const PolicyArg
   r.fetch_all(row);
   const float c = (float)(a.inv_t * kLog2e64), at = Elem<DT>::get(row, y);
   double sums[2];
-  const float m = row_sums<W, !GRAD>(r, row, c, [](int, float (&)[Elem<DT>::kPerVec]) {}, slots, sums, -INFINITY);
+  float tops[1];
+  const float m = row_sums<W, !GRAD>(r, row, c, [](int, float (&)[Elem<DT>::kPerVec]) {}, slots, sums, tops);
   team_sum<W>(sums, slots);
   const bool empty = sums[0] == 0.0;
   const double w = a.weights != nullptr ? (double)a.weights[n] : 1.0;
@@ -463,8 +475,6 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
   for (int i = tid; i < bits_words(V, NT); i += NT) listed[i] = 0;
   // A vector's tokens have neighbouring bits, from a multiple of E on.
   const auto bit_of = [&](int id) { return id >= r.head ? id - r.head : V - r.head + id; };
-  // The list, and its largest value.
-  float tm = -INFINITY;
   bool again = false;
   __syncthreads();
   for (int j = tid; j < K; j += NT) {
@@ -494,16 +504,19 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
       if (drop[i]) list[i * NT + tid].id = -1;
     __syncthreads();
   }
-  float top = -INFINITY;
+  // The largest logits outside the list and in it, and the list's largest value.
+  float tops[3] = {-INFINITY, -INFINITY, -INFINITY};
   for (int j = tid; j < K; j += NT) {
     if (list[j].id < 0) continue;
-    top = fmaxf(top, list[j].x);
-    tm = fmaxf(tm, (float)list[j].t);
+    tops[1] = fmaxf(tops[1], list[j].x);
+    tops[2] = fmaxf(tops[2], (float)list[j].t);
   }
-  // Sums over the tokens outside the list; those of the list are added apart,
-  // so that a small mass outside is no difference of large ones.
+  // The sum So over the tokens outside the list, relative to the largest of those, m_o:
+  // however far they lie below the list, their mass has a logarithm and each has its
+  // share e / So of it. Those of the list are added apart, so that a small mass
+  // outside is no difference of large ones.
   double so_t[2];
-  const float m = row_sums<W, !GRAD>(r, row, c, [&](int v, float (&x)[E]) {
+  const float m_o = row_sums<W, !GRAD>(r, row, c, [&](int v, float (&x)[E]) {
     const int bit = v < r.whole || r.id >= r.loose ? v * E : bit_of(r.loose_of());
     uint32_t hit;
     if constexpr (E == 8) hit = v < r.whole ? listed8[v] : listed[bit / 32] >> (bit % 32) & 1u;
@@ -511,12 +524,9 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
     if (hit == 0) return;
 #pragma unroll
     for (int k = 0; k < E; ++k) x[k] = hit >> k & 1 ? -INFINITY : x[k];
-  }, slots, so_t, top);
-  if (a.kind == RP_DISTILL_TOPK) {
-    __syncthreads();
-    tm = team_max<W>(tm, slots);
-  }
-  // so, and over the list: e, P, and the loss's terms but for ln S:
+  }, slots, so_t, tops);
+  const float m = fmaxf(m_o, tops[1]), tm = tops[2];
+  // So, and over the list: e, P, and the loss's terms but for ln S:
   // P (ln P - z) with P = exp(t) / total, or e (z - ln P).
   double sums[4] = {so_t[0], 0.0, 0.0, 0.0};
   for (int j = tid; j < K; j += NT) {
@@ -532,22 +542,23 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
     else sums[3] += P == 0.0 ? 0.0 : P * (t - z);
   }
   team_sum<W>(sums, slots);
-  const double so = sums[0], s = so + sums[1], P_sum = sums[2];
+  const double So = sums[0], far = ((double)m_o - (double)m) * a.inv_t, so = So * exp(far), s = so + sums[1];
+  const double P_sum = sums[2];
   const bool empty = s == 0.0;
+  const bool outside = !(So == 0.0);  // a NaN stays
   const double ln_s = log(s), qo = so / s, per = (double)w * a.inv_t;
-  const double rest = fmax(1.0 - P_sum, 0x1p-24), gap = log(qo / rest);
-  const bool outside = !(qo == 0.0);  // a NaN stays
-  double loss, whole = 1.0, others;
+  const double rest = fmax(1.0 - P_sum, 0x1p-24), gap = log(So) + far - ln_s - log(rest);
+  double loss, whole = 1.0, others;  // others: a token outside has e / So of it as its gradient
   if (a.kind == RP_DISTILL_TOPK) {
     loss = P_sum > 0.0 ? sums[3] / P_sum - log(P_sum) + ln_s : 0.0 * s;
-    others = P_sum > 0.0 ? 1.0 : 0.0;  // an empty list teaches nothing
+    others = P_sum > 0.0 ? qo : 0.0;  // an empty list teaches nothing
   } else if (a.kind == RP_DISTILL_TAIL) {
     loss = sums[3] + P_sum * ln_s - (outside ? rest * gap : 0.0);
     whole = P_sum + (outside ? rest : 0.0);
-    others = outside ? whole - rest / qo : 0.0;
+    others = whole * qo - rest;
   } else {
     loss = (sums[3] - ln_s * sums[1]) / s + (outside ? qo * gap : 0.0);
-    others = outside ? gap - loss : 0.0;
+    others = qo * (gap - loss);
   }
   if (tid == 0) a.losses[n] = empty ? 0.f : (float)((double)w * loss);
   for (int j = tid; GRAD && j < K; j += NT) {
@@ -564,8 +575,9 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
       r.zero(out);
       return;
     }
-    const float alpha = (float)(per * others / s);
-    r.store(row, out, [&](float x) { return fast_exp2((x - m) * c) * alpha; });
+    // With nothing outside every other token is masked: 0, or NaN in a row that has one.
+    const float alpha = outside ? (float)(per * others / So) : (float)(0.0 * s);
+    r.store(row, out, [&](float x) { return fast_exp2((x - m_o) * c) * alpha; });
     __syncthreads();  // the list's elements come after their vectors
     for (int j = tid; j < K; j += NT)
       if (list[j].id >= 0) put_elem<DT>(out, list[j].id, list[j].x);

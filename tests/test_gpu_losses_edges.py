@@ -1,0 +1,82 @@
+"""Losses over rows of logits on the GPU at the ends of their ranges, against the float64 oracle: a list far above all other
+tokens."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from tests.rows_util import U, guarded, half_step, lse_bound, say
+from tests.test_gpu_losses import _distill_run, _near
+
+pytestmark = pytest.mark.gpu
+
+
+def _far_check(x, dtype, ids, values, kind, w, T, got, what):
+    """From logarithms: with m_o the largest logit outside the list and S_o the sum of exp((x - m_o) / T) there (off by
+    lse_bound relative, its terms by (3 z + 4) u), q_o = S_o exp((m_o - m) / T) / s and the gradient outside is
+    w / T e_i / S_o times a number of the row that is as exact as q_o; sums over the list are in 64 bits."""
+    V, lb = x.shape[1], lse_bound(x.shape[1])
+    loss, grad = oracle.distill_loss(x, ids, values, kind=kind, weights=w, temperature=T)
+    tiny = 2.0 ** -25 if dtype == "f16" else 1e-37
+    for r in range(len(x)):
+        others = np.isfinite(x[r])
+        others[ids[r]] = False
+        z = np.where(others, (x[r][others].max() - np.where(others, x[r], 0.0)) / T, 0.0)
+        l = oracle.rows.log_softmax(x[r], T)
+        t, lq = values[r].astype(np.float64), l[ids[r]]
+        qo, lqo = np.exp(l[others]).sum(), np.abs(oracle.rows.log_sum(l[others]))
+        if kind == "topk":
+            size, listed = 1.0, np.exp(lq)
+        elif kind == "tail":
+            size, listed = np.exp(t).sum() + 1.0, np.exp(lq) * (np.exp(t).sum() + 1)
+        else:
+            size = (np.exp(lq) * (np.abs(lq) + np.abs(t) + 1)).sum() + qo * (lqo + 17)
+            listed = np.exp(lq) * (np.abs(lq) + np.abs(t) + 1 + size)
+        _near(got[0][r:r + 1], loss[r:r + 1], w[r] * 2 * size * lb + U * abs(loss[r]) + w[r] * 1e-12, f"{what} losses")
+        bound = (3 * z + 8) * U * np.abs(grad[r]) + 2 * lb * np.abs(grad[r])
+        if kind != "topk":
+            share = np.where(others, np.exp(-z), 0.0)
+            bound += w[r] / T * share / share.sum() * qo * 2 * lb * (2.0 if kind == "tail" else lqo + 18 + size)
+        bound[ids[r]] += w[r] / T * listed * 2 * lb
+        _near(got[1][r], grad[r], bound + half_step(dtype) * 1.01 * np.abs(grad[r]) + tiny, f"{what} dlogits")
+
+
+@pytest.mark.parametrize("kind", ["topk", "tail", "reverse"])
+@pytest.mark.parametrize("V,dtype,masked", [(8, "f32", 0), (3000, "bf16", 7), (40001, "f32", 100), (140000, "f16", 0)])
+def test_tokens_far_below_the_list(V, dtype, masked, kind):
+    """What is outside the list keeps its class however small its mass: gaps of 80 and more, also through temperatures
+    below 1, and a weight over T that a factor of the row's maximum would take past fp32's range."""
+    say(f"far outside {V} {dtype} masked {masked} {kind}")
+    rng = np.random.default_rng(V)
+    for gap, T, weight in ((30.0, 1.0, 1.0), (80.0, 1.0, 1.0), (87.0, 1.0, 30.0), (90.0, 1.0, 1.0), (103.0, 1.0, 500.0),
+                           (200.0, 1.0, 1.0), (900.0, 1.0, 1.0), (20.0, 0.2, 3.0), (9.0, 0.1, 10.0), (90.0, 0.1, 1.0)):
+        n, k = 3, min(3, V // 4)
+        view, _ = guarded(n, V, dtype)
+        x = 0.5 * T * rng.standard_normal((n, V))
+        ids = np.stack([rng.permutation(V - masked)[:k] for _ in range(n)]).astype(np.int32)
+        np.put_along_axis(x, ids.astype(np.int64), gap + 0.2 * T * rng.random((n, k)), 1)
+        if masked:
+            x[:, V - masked:] = -np.inf
+        view.copy_(torch.from_numpy(x))
+        x = view.double().cpu().numpy()
+        values = np.log(np.full((n, k), 0.9 / k) * (0.9 + 0.1 * rng.random((n, k)))).astype(np.float32)
+        w = np.full(n, weight, np.float32)
+        grad, _ = guarded(n, V, dtype)
+        got = _distill_run(view, ids, values, kind, w, T, grad)
+        _far_check(x, dtype, ids, values, kind, w.astype(np.float64), T, got, f"gap {gap} T {T}")
+        alone = _distill_run(view, ids, values, kind, w, T, None)
+        assert np.array_equal(alone[0], got[0])
+
+
+def test_a_divergence_beside_a_far_outside():
+    """One listed token of probability 1/2 that the student takes for certain: the loss is 43, not below 0."""
+    say("far outside, by hand")
+    view = torch.zeros(1, 8, device="cuda")
+    view[0, 0] = 90.0
+    ids, values = np.zeros((1, 1), np.int32), np.full((1, 1), math.log(0.5), np.float32)
+    grad, _ = guarded(1, 8, "f32")
+    got = _distill_run(view, ids, values, "tail", None, 1.0, grad)
+    assert abs(got[0][0] - (math.log(0.5) + 0.5 * (90 - math.log(7)))) < 1e-4
+    assert np.abs(got[1][0] - np.array([0.5] + [-0.5 / 7] * 7)).max() < 1e-6
