@@ -588,7 +588,8 @@ rp_status rp_policy_loss(const rp_logits* logits, const rp_policy_batch* batch,
  *   RP_DISTILL_REVERSE: the same classes,
  *     loss = sum q (ln q - ln P) + q_o (ln q_o - ln P_o).
  * A class outside to which the student gives nothing (every other token masked)
- * is left out. */
+ * is left out. A NaN or +inf among the values that count leaves the row's loss
+ * no finite number. */
 typedef enum {
   RP_DISTILL_TOPK = 0,
   RP_DISTILL_TAIL = 1,

@@ -141,6 +141,7 @@ def policy_loss(x, tokens, old, advantages, *, row_seq=None, weights=None, ref=N
     return loss, lp, H, grad
 
 
+@np.errstate(invalid="ignore", over="ignore")
 def distill_loss(x, ids, values, *, kind="tail", weights=None, temperature=1.0):
     """losses, dlogits."""
     n, V = x.shape
@@ -167,7 +168,7 @@ def distill_loss(x, ids, values, *, kind="tail", weights=None, temperature=1.0):
             t = t - t.max()
             lp = t - math.log(math.fsum(np.exp(t)))
             P = np.exp(lp)
-            value, d = math.fsum(np.where(P > 0, P * (lp - lq), 0.0)), q.copy()
+            value, d = math.fsum(np.where(P == 0, 0.0, P * (lp - lq))), q.copy()
             d[at] -= P
         else:
             P = np.exp(t)
@@ -179,14 +180,13 @@ def distill_loss(x, ids, values, *, kind="tail", weights=None, temperature=1.0):
             outside, out = log_out > -math.inf, math.exp(log_out)
             gap = log_out - math.log(rest) if outside else 0.0
             if kind == "tail":
-                value = math.fsum(np.where(P > 0, P * (t - lq), 0.0)) - (rest * gap if outside else 0.0)
+                value = math.fsum(np.where(P == 0, 0.0, P * (t - lq))) - (rest * gap if outside else 0.0)
                 whole = math.fsum(P) + (rest if outside else 0.0)
                 d = whole * q - rest * np.exp(np.where(others, l - log_out, -np.inf)) if outside else np.zeros(V)
                 d[at] = whole * q[at] - P
             else:
-                with np.errstate(invalid="ignore"):
-                    value = math.fsum(np.where(q[at] > 0, q[at] * (lq - t), 0.0)) + out * gap
-                    d = q * (gap - value) if outside else np.zeros(V)
-                    d[at] = np.where(q[at] > 0, q[at] * (lq - t - value), 0.0)
+                value = math.fsum(np.where(q[at] == 0, 0.0 * P, q[at] * (lq - t))) + out * gap
+                d = q * (gap - value) if outside else np.zeros(V)
+                d[at] = np.where(q[at] > 0, q[at] * (lq - t - value), 0.0)
         loss[r], grad[r] = w * value, w / temperature * d
     return loss, grad

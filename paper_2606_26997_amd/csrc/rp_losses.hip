@@ -538,7 +538,8 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
     if (a.kind != RP_DISTILL_REVERSE) list[j].t = P;
     sums[1] += e;
     sums[2] += P;
-    if (a.kind == RP_DISTILL_REVERSE) sums[3] += e == 0.0 ? 0.0 : e * (z - t);
+    // (0 P: a teacher's NaN or +inf stays.)
+    if (a.kind == RP_DISTILL_REVERSE) sums[3] += e == 0.0 ? 0.0 * P : e * (z - t);
     else sums[3] += P == 0.0 ? 0.0 : P * (t - z);
   }
   team_sum<W>(sums, slots);
@@ -547,11 +548,13 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
   const bool empty = s == 0.0;
   const bool outside = !(So == 0.0);  // a NaN stays
   const double ln_s = log(s), qo = so / s, per = (double)w * a.inv_t;
-  const double rest = fmax(1.0 - P_sum, 0x1p-24), gap = log(So) + far - ln_s - log(rest);
+  const double left = 1.0 - P_sum, rest = left < 0x1p-24 ? 0x1p-24 : left;  // a NaN stays here too
+  const double gap = log(So) + far - ln_s - log(rest);
   double loss, whole = 1.0, others;  // others: a token outside has e / So of it as its gradient
   if (a.kind == RP_DISTILL_TOPK) {
-    loss = P_sum > 0.0 ? sums[3] / P_sum - log(P_sum) + ln_s : 0.0 * s;
-    others = P_sum > 0.0 ? qo : 0.0;  // an empty list teaches nothing
+    const bool lists = !(P_sum == 0.0);  // an empty list teaches nothing
+    loss = lists ? sums[3] / P_sum - log(P_sum) + ln_s : 0.0 * s;
+    others = lists ? qo : 0.0;
   } else if (a.kind == RP_DISTILL_TAIL) {
     loss = sums[3] + P_sum * ln_s - (outside ? rest * gap : 0.0);
     whole = P_sum + (outside ? rest : 0.0);

@@ -1,5 +1,5 @@
 """Losses over rows of logits on the GPU at the ends of their ranges, against the float64 oracle: a list far above all other
-tokens."""
+tokens, a teacher's values that are no numbers."""
 import math
 
 import numpy as np
@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import oracle
-from tests.rows_util import U, guarded, half_step, lse_bound, say
+from tests.rows_util import U, guarded, half_step, logits, lse_bound, say
 from tests.test_gpu_losses import _distill_run, _near
 
 pytestmark = pytest.mark.gpu
@@ -80,3 +80,27 @@ def test_a_divergence_beside_a_far_outside():
     got = _distill_run(view, ids, values, "tail", None, 1.0, grad)
     assert abs(got[0][0] - (math.log(0.5) + 0.5 * (90 - math.log(7)))) < 1e-4
     assert np.abs(got[1][0] - np.array([0.5] + [-0.5 / 7] * 7)).max() < 1e-6
+
+
+@pytest.mark.parametrize("kind", ["topk", "tail", "reverse"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_teachers_values_that_are_no_numbers(kind, bad):
+    """A NaN or +inf among a teacher's values is no empty list: the loss is not finite, nor is the entry's gradient."""
+    say(f"teacher of {bad} {kind}")
+    rng = np.random.default_rng(1)
+    n, V, k = 4, 600, 8
+    x, view, _ = logits(rng, n, V, "f32")
+    ids = np.stack([rng.permutation(V)[:k] for _ in range(n)]).astype(np.int32)
+    values = np.log(np.full((n, k), 0.1)).astype(np.float32)
+    values[0, 0] = values[1, k - 1] = values[2, 3] = bad
+    view[2, int(ids[2, 3])] = -math.inf      # an entry that the student rules out
+    values[2, 5] = -math.inf
+    grad, _ = guarded(n, V, "f32")
+    loss, g = _distill_run(view, ids, values, kind, None, 1.0, grad)
+    want, _ = oracle.distill_loss(view.double().cpu().numpy(), ids, values, kind=kind)
+    assert not np.isfinite(loss[:3]).any() and np.isfinite(loss[3]), loss
+    assert not np.isfinite(want[:3]).any() and np.isfinite(want[3])
+    for r, j in ((0, 0), (1, k - 1)):
+        assert not np.isfinite(g[r, ids[r, j]])
+    assert np.isfinite(g[3]).all()
+    assert np.array_equal(_distill_run(view, ids, values, kind, None, 1.0, None)[0], loss, equal_nan=True)

@@ -29,3 +29,12 @@ def test_a_class_outside_far_below_the_list(rng, gap, kind):
     (g,) = torch.autograd.grad(ref.sum(), t)
     assert np.allclose(loss, ref.detach().numpy(), rtol=1e-13, atol=1e-13)
     assert np.allclose(grad, g.numpy(), rtol=1e-12, atol=1e-13)
+
+
+@pytest.mark.parametrize("kind", ["topk", "tail", "reverse"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_teachers_values_that_are_no_numbers(rng, bad, kind):
+    x = rng.standard_normal((2, 9))
+    x[1, 4] = -np.inf
+    loss, _ = oracle.distill_loss(x, np.array([[1, 4], [1, 4]]), np.array([[-1.0, bad], [-1.0, bad]]), kind=kind)
+    assert not np.isfinite(loss).any()
