@@ -21,6 +21,9 @@ constexpr float kLeast = -1e30f;
 // summed again without products that overflow (row_sums).
 constexpr float kMostRef = 1e36f;
 
+// log2(e) / T in fp32, above 0 however large T is: c times -inf has to be -inf.
+__device__ inline float scale_of(double inv_t) { return fmaxf((float)(inv_t * kLog2e64), 0x1p-149f); }
+
 // A thread's sums relative to 2^r: of e and e d over the vector with its largest
 // logit (group, group_t) and over all others (rest, rest_t). They are apart so
 // that the one vector can be summed again in 64 bits (join): in a row in which
@@ -333,7 +336,7 @@ __global__ __launch_bounds__(threads_of<W>()) void logprobs_kernel(const Logprob
     }
     return;
   }
-  const float c = (float)(a.inv_t * kLog2e64), at = Elem<DT>::get(row, y);
+  const float c = scale_of(a.inv_t), at = Elem<DT>::get(row, y);
   r.fetch_all(row);
   double sums[2];
   float tops[1];
@@ -369,7 +372,7 @@ __global__ __launch_bounds__(threads_of<W>()) void policy_kernel(const PolicyArg
     return;
   }
   r.fetch_all(row);
-  const float c = (float)(a.inv_t * kLog2e64), at = Elem<DT>::get(row, y);
+  const float c = scale_of(a.inv_t), at = Elem<DT>::get(row, y);
   double sums[2];
   float tops[1];
   const float m = row_sums<W, !GRAD>(r, row, c, [](int, float (&)[Elem<DT>::kPerVec]) {}, slots, sums, tops);
@@ -460,7 +463,7 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
   Entry* list = reinterpret_cast<Entry*>(dynamic);
   uint32_t* listed = reinterpret_cast<uint32_t*>(list + K);  // a bit per token of the vocabulary
   const uint8_t* listed8 = reinterpret_cast<const uint8_t*>(listed);
-  const float c = (float)(a.inv_t * kLog2e64);
+  const float c = scale_of(a.inv_t);
   const int n = blockIdx.x;
   const char* row = row_of<DT>(a.logits, n);
   Row<DT, W, NV> r(V, row);

@@ -1,5 +1,6 @@
 """Losses over rows of logits on the GPU at the ends of their ranges, against the float64 oracle: a list far above all other
-tokens, a teacher's values that are no numbers."""
+tokens, a teacher's values that are no numbers, temperatures past
+fp32's range."""
 import math
 
 import numpy as np
@@ -7,8 +8,8 @@ import pytest
 import torch
 
 import oracle
-from tests.rows_util import U, guarded, half_step, logits, lse_bound, say
-from tests.test_gpu_losses import _distill_run, _near
+from tests.rows_util import U, dev, empty, entropy_bound, guarded, half_step, logits, lse_bound, say, workspace
+from tests.test_gpu_losses import _distill_run, _near, _policy_check, _policy_run
 
 pytestmark = pytest.mark.gpu
 
@@ -104,3 +105,31 @@ def test_teachers_values_that_are_no_numbers(kind, bad):
         assert not np.isfinite(g[r, ids[r, j]])
     assert np.isfinite(g[3]).all()
     assert np.array_equal(_distill_run(view, ids, values, kind, None, 1.0, None)[0], loss, equal_nan=True)
+
+
+@pytest.mark.parametrize("T", [1e39, 1e45, 1e46, 1e60, 1e300])
+@pytest.mark.parametrize("V,dtype", [(50, "bf16"), (3001, "f32"), (40001, "f16")])
+def test_temperatures_past_fp32(V, dtype, T):
+    """log2(e) / T passes fp32's least number: tokens that can occur become equally likely, the others stay out."""
+    import paper_2606_26997_amd as rp
+    say(f"temperature {T} {V} {dtype}")
+    rng = np.random.default_rng(V)
+    n = 3
+    x, view, _ = logits(rng, n, V, dtype, masked=5)
+    tokens = np.array([int(np.flatnonzero(np.isfinite(r))[3]) for r in x], np.int32)
+    lp, H = empty(n), empty(n)
+    rp.token_logprobs(view, dev(tokens, torch.int32), lp, H, temperature=T, workspace=workspace(view))
+    want = oracle.token_logprobs(x, tokens, T)
+    _near(lp.double().cpu(), want[0], lse_bound(V) + U * np.abs(want[0]), "logprobs")
+    _near(H.double().cpu(), want[1], entropy_bound(V) + U * np.abs(want[1]), "entropy")
+    case = (tokens, want[0].astype(np.float32), want[0].astype(np.float32), np.zeros(n, np.int32), np.ones(1, np.float32),
+            np.ones(n, np.float32))
+    grad, _ = guarded(n, V, dtype)
+    _policy_check(x, view, dtype, T, case, _policy_run(view, dtype, T, case, 0.05, 0.01, grad), 0.05, 0.01)
+    ids = np.stack([np.flatnonzero(np.isfinite(r))[:4] for r in x]).astype(np.int32)
+    values = np.log(np.full((n, 4), 0.2)).astype(np.float32)
+    for kind in ("topk", "tail", "reverse"):
+        loss, g = _distill_run(view, ids, values, kind, None, T, grad)
+        want, wg = oracle.distill_loss(x, ids, values, kind=kind, temperature=T)
+        _near(loss, want, 4 * lse_bound(V) * (1 + math.log(V)) + U * np.abs(want), kind + " losses")
+        assert np.abs(g - wg).max() <= 1e-37
