@@ -24,6 +24,15 @@ constexpr float kMostRef = 1e36f;
 // log2(e) / T in fp32, above 0 however large T is: c times -inf has to be -inf.
 __device__ inline float scale_of(double inv_t) { return fmaxf((float)(inv_t * kLog2e64), 0x1p-149f); }
 
+// d = (x - max) c. Where c is below 1 by half the difference, which is as exact and does
+// not pass fp32's range: at T = 1e38 logits of 3e38 and -3e38 both count.
+struct Below {
+  float half, half_max, c;
+  __device__ inline Below(float max, float scale)
+      : half(scale < 1.f ? 0.5f : 1.f), half_max(max * half), c(scale < 1.f ? scale * 2.f : scale) {}
+  __device__ inline float operator()(float x) const { return fmaf(x, half, -half_max) * c; }
+};
+
 // A thread's sums relative to 2^r: of e and e d over the vector with its largest
 // logit (group, group_t) and over all others (rest, rest_t). They are apart so
 // that the one vector can be summed again in 64 bits (join): in a row in which
@@ -84,9 +93,10 @@ __device__ inline void join(const Stats& a, float max, float c, double& s, doubl
   t = f * ((double)a.rest_t + (double)shift * (double)a.rest);
   float x[E];
   reload(a.at, x);
+  const Below below(max, c);
 #pragma unroll
   for (int k = 0; k < E; ++k) {
-    const float d = (x[k] - max) * c, e = fast_exp2(d);
+    const float d = below(x[k]), e = fast_exp2(d);
     s += (double)e;
     t += (double)e * (double)fmaxf(d, kLeast);
   }
@@ -303,11 +313,12 @@ __device__ inline float row_sums(R& r, const char* row, float c, const Masked& m
     join<E>(st, m, c, sums[0], sums[1], reload);
   } else {
     sums[0] = sums[1] = 0.0;
+    const Below below(m, c);
     for (int v = r.id; v < r.whole + (r.id < r.loose ? R::NT : 0); v += R::NT) {
       float x[E];
       reload(v < r.whole ? v : r.whole, x);
       for (int k = 0; k < E; ++k) {
-        const float d = (x[k] - m) * c, e = fast_exp2(d);
+        const float d = below(x[k]), e = fast_exp2(d);
         sums[0] += (double)e;
         sums[1] += (double)e * (double)fmaxf(d, kLeast);
       }
@@ -426,8 +437,9 @@ __global__ __launch_bounds__(threads_of<W>()) void policy_kernel(const PolicyArg
       beta = slots.out[1];
       own = slots.out[2];
     }
+    const Below below(m, c);
     r.store(row, out, [&](float x) {
-      const float d = (x - m) * c;
+      const float d = below(x);
       return fast_exp2(d) * fmaf(beta, fmaxf(d, kLeast), alpha);
     });
     // The token's own element comes after its vector, from the same thread.
@@ -583,7 +595,8 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
     }
     // With nothing outside every other token is masked: 0, or NaN in a row that has one.
     const float alpha = outside ? (float)(per * others / So) : (float)(0.0 * s);
-    r.store(row, out, [&](float x) { return fast_exp2((x - m_o) * c) * alpha; });
+    const Below below(m_o, c);
+    r.store(row, out, [&](float x) { return fast_exp2(below(x)) * alpha; });
     __syncthreads();  // the list's elements come after their vectors
     for (int j = tid; j < K; j += NT)
       if (list[j].id >= 0) put_elem<DT>(out, list[j].id, list[j].x);

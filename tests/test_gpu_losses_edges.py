@@ -1,6 +1,5 @@
 """Losses over rows of logits on the GPU at the ends of their ranges, against the float64 oracle: a list far above all other
-tokens, a teacher's values that are no numbers, temperatures past
-fp32's range."""
+tokens, a teacher's values that are no numbers, temperatures past fp32's range, logits further apart than that."""
 import math
 
 import numpy as np
@@ -8,8 +7,8 @@ import pytest
 import torch
 
 import oracle
-from tests.rows_util import U, dev, empty, entropy_bound, guarded, half_step, logits, lse_bound, say, workspace
-from tests.test_gpu_losses import _distill_run, _near, _policy_check, _policy_run
+from tests.rows_util import U, dev, empty, entropy_bound, f32, guarded, half_step, logits, lse_bound, say, workspace
+from tests.test_gpu_losses import _distill_run, _near, _policy_case, _policy_check, _policy_run
 
 pytestmark = pytest.mark.gpu
 
@@ -133,3 +132,43 @@ def test_temperatures_past_fp32(V, dtype, T):
         want, wg = oracle.distill_loss(x, ids, values, kind=kind, temperature=T)
         _near(loss, want, 4 * lse_bound(V) * (1 + math.log(V)) + U * np.abs(want), kind + " losses")
         assert np.abs(g - wg).max() <= 1e-37
+
+
+@pytest.mark.parametrize("V", [8, 5000, 50000])
+def test_logits_further_apart_than_fp32_reaches(V):
+    """Logits between -3.3e38 and 3.3e38 at temperatures where each of them counts. |z| is at most 6.6e38 / T, not ln V on
+    average; a weight of T / 10 makes the gradient a number."""
+    import paper_2606_26997_amd as rp
+    say(f"logits of +-3.3e38, {V}")
+    rng = np.random.default_rng(V)
+    n = 3
+    view, _ = guarded(n, V, "f32")
+    ends = np.where(rng.random((n, V)) < 0.5, 3.3e38, -3.3e38)
+    view.copy_(torch.from_numpy(ends * (1 - 0.3 * rng.random((n, V)))))
+    view[2, 7] = -math.inf
+    x = view.double().cpu().numpy()
+    for T in (4e37, 1e38, 1e39):
+        case = list(_policy_case(rng, x, T, n))
+        case[5] = np.full(n, T / 10, np.float32)
+        far = 6.6e38 / T
+        sums = lse_bound(V) + (3 * far + 2) * U
+        lp, H = empty(n), empty(n)
+        rp.token_logprobs(view, dev(case[0], torch.int32), lp, H, temperature=T, workspace=workspace(view))
+        want = oracle.token_logprobs(x, case[0], T)
+        _near(lp.double().cpu(), want[0], sums + U * np.abs(want[0]), f"T {T} logprobs")
+        _near(H.double().cpu(), want[1], (1 + far) * sums + U * np.abs(want[1]), f"T {T} entropy")
+        grad, _ = guarded(n, V, "f32")
+        got = _policy_run(view, "f32", T, case, 0.05, 0.0, grad)["grad"]
+        want = oracle.policy_loss(x, case[0], case[1].astype(np.float64), case[4], row_seq=case[3],
+                                  weights=case[5].astype(np.float64), ref=case[2].astype(np.float64), temperature=T,
+                                  clip_low=0.2, clip_high=0.25, kl_beta=0.05)[3]
+        # Terms off by (3 z + 8) u, the row's sum and, with a slope of at most 3.3, its factor by `sums`.
+        slack = (3 * far + 10) * U + 5 * sums
+        _near(got, want, slack * np.abs(want) + 0.1 * 4 * sums * np.abs(want / want.max()) + 1e-37, f"T {T} dlogits")
+        ids, values = np.array([[1, 2]] * n, np.int32), np.log(np.full((n, 2), 0.3)).astype(np.float32)
+        for kind in ("topk", "tail", "reverse"):
+            loss, g = _distill_run(view, ids, values, kind, case[5], T, grad)
+            want = oracle.distill_loss(x, ids, values, kind=kind, weights=case[5].astype(np.float64), temperature=T)
+            # At T = 1e39 losses of 1e38 times 7 round to infinity.
+            _near(loss, f32(want[0]), case[5] * sums * (4 + 2 * far) + 2 * U * np.abs(want[0]), f"T {T} {kind}")
+            assert np.abs(g - want[1]).max() <= 0.1 * (3 * far + 10 + far) * 4 * sums, (T, kind)
