@@ -548,8 +548,9 @@ rp_status rp_token_logprobs(const rp_logits* logits, const int32_t* tokens, doub
  * [0, num_advantages), are skipped: their logits are not read, and loss,
  * log-probability, entropy and gradient are 0. A weight of 0 gives loss and
  * gradient 0 whatever else the row holds. A token whose own logit is -inf has
- * l = -inf and r = 0; there k has no finite value, and with kl_beta the loss is
- * not a number and the gradient not finite. */
+ * l = -inf and r = 0 (whatever old_logprobs holds); there k has no finite value,
+ * and with kl_beta the loss is not a number and the gradient not finite. Where
+ * r passes the range of numbers, r A with A = 0 is 0. */
 typedef struct {
   const int32_t* tokens;        /* [num_rows] */
   const float* old_logprobs;    /* [num_rows], of the policy that drew the tokens */

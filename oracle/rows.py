@@ -108,6 +108,7 @@ def token_logprobs(x, tokens, temperature=1.0):
     return lp, H
 
 
+@np.errstate(over="ignore")
 def policy_loss(x, tokens, old, advantages, *, row_seq=None, weights=None, ref=None, temperature=1.0, clip_low=0.2,
                 clip_high=0.2, kl_beta=0.0, entropy_coef=0.0):
     """losses, logprobs, entropy, dlogits."""
@@ -126,8 +127,8 @@ def policy_loss(x, tokens, old, advantages, *, row_seq=None, weights=None, ref=N
             continue
         l, A = log_softmax(x[r], temperature), adv[seq[r]]
         p = np.exp(l)
-        with np.errstate(over="ignore"):
-            ratio = float(np.exp(l[y] - old[r]))
+        # r of a token that cannot occur is 0; an advantage of 0 has no surrogate, however large r is.
+        ratio = 0.0 if l[y] == -np.inf else min(float(np.exp(l[y] - old[r])), np.finfo(np.float64).max)
         free, held = ratio * A, min(max(ratio, 1 - clip_low), 1 + clip_high) * A
         value, g = -min(free, held) - entropy_coef * H[r], -free if free <= held else 0.0
         if kl_beta:

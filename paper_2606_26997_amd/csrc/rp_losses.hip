@@ -398,7 +398,10 @@ __global__ __launch_bounds__(threads_of<W>()) void policy_kernel(const PolicyArg
     const double lp = empty ? -INFINITY : ((double)at - (double)m) * a.inv_t - ln_s;
     const double H = empty ? 0.0 : ln_s - kLn2_64 * sums[1] / sums[0];
     const double A = (double)a.advantages[seq], gap = a.ref_logprobs != nullptr ? (double)a.ref_logprobs[n] - lp : 0.0;
-    const double e = exp(r.id == 0 ? lp - (double)a.old_logprobs[n] : r.id == 1 ? gap : lp);
+    // A token that cannot occur has r = 0, whatever the old policy gave it; r stays finite,
+    // so that an advantage of 0 leaves no surrogate (a NaN passes both).
+    const double log_r = lp == -INFINITY ? lp : lp - (double)a.old_logprobs[n];
+    const double e = exp(r.id == 0 ? (log_r > 700.0 ? 700.0 : log_r) : r.id == 1 ? gap : lp);
     const double ratio = __shfl(e, 0), e_gap = __shfl(e, 1), p = __shfl(e, 2);
     // 1 - p, also where lp is small: -lp - lp^2 / 2 - lp^3 / 6 is 4e-14 off at 1e-4.
     const double not_p = lp > -1e-4 ? -lp * (1.0 + lp * (0.5 + lp * (1.0 / 6.0))) : 1.0 - p;

@@ -1,5 +1,6 @@
 """Losses over rows of logits on the GPU at the ends of their ranges, against the float64 oracle: a list far above all other
-tokens, a teacher's values that are no numbers, temperatures past fp32's range, logits further apart than that."""
+tokens, a teacher's values that are no numbers, temperatures past fp32's range, logits further apart than that,
+ratios that are no finite numbers."""
 import math
 
 import numpy as np
@@ -172,3 +173,23 @@ def test_logits_further_apart_than_fp32_reaches(V):
             # At T = 1e39 losses of 1e38 times 7 round to infinity.
             _near(loss, f32(want[0]), case[5] * sums * (4 + 2 * far) + 2 * U * np.abs(want[0]), f"T {T} {kind}")
             assert np.abs(g - want[1]).max() <= 0.1 * (3 * far + 10 + far) * 4 * sums, (T, kind)
+
+
+def test_ratios_that_are_no_finite_numbers():
+    """A token that cannot occur has r = 0 whatever the old policy gave it, and an advantage of 0 has no surrogate, also
+    beside a ratio past fp64's range."""
+    say("ratios")
+    n, V = 8, 40
+    x, view, _ = logits(np.random.default_rng(3), n, V, "f32")
+    view[0, 5] = view[1, 5] = -math.inf
+    view[6, 9] = math.nan
+    x = view.double().cpu().numpy()
+    tokens = np.full(n, 5, np.int32)
+    old = np.array([-np.inf, -1.0, -np.inf, -np.inf, -1e30, -2.0, -1.0, -2.0], np.float32)
+    adv = np.array([1.0, 1.0, 0.0, 1.0, 0.0, 0.0, 0.0, -1.0], np.float32)
+    case = (tokens, old, np.zeros(n, np.float32), np.arange(n, dtype=np.int32), adv, np.ones(n, np.float32))
+    grad, _ = guarded(n, V, "f32")
+    got = _policy_run(view, "f32", 1.0, case, 0.0, 0.01, grad)
+    fine = np.arange(n) != 6
+    assert np.isfinite(got["losses"][fine]).all() and np.isfinite(got["grad"][fine]).all(), got
+    _policy_check(x, view, "f32", 1.0, case, got, 0.0, 0.01)

@@ -38,3 +38,12 @@ def test_teachers_values_that_are_no_numbers(rng, bad, kind):
     x[1, 4] = -np.inf
     loss, _ = oracle.distill_loss(x, np.array([[1, 4], [1, 4]]), np.array([[-1.0, bad], [-1.0, bad]]), kind=kind)
     assert not np.isfinite(loss).any()
+
+
+def test_ratios_that_are_no_finite_numbers(rng):
+    """A token that cannot occur has r = 0 whatever the old policy gave it; an advantage of 0 has no surrogate."""
+    x = rng.standard_normal((4, 9))
+    x[0, 4] = x[1, 4] = -np.inf
+    old, adv = np.array([-np.inf, -1.0, -np.inf, -np.inf]), np.array([1.0, 1.0, 0.0, 2.0])
+    loss, _, _, grad = oracle.policy_loss(x, np.full(4, 4), old, adv)
+    assert loss.tolist() == [0.0, 0.0, 0.0, -1.2 * 2.0] and not grad.any()
