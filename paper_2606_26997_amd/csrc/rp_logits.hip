@@ -67,9 +67,12 @@ rp_status check_gradient(const Rows& r, void* dlogits, int64_t stride) {
       return fail(RP_ERR_INVALID_ARG, "dlogits in the logits' place needs their stride");
     return RP_OK;
   }
-  const auto span = [&](int64_t s) { return (uintptr_t)(((r.args.rows - 1) * s + r.args.vocab) * r.bytes); };
-  const uintptr_t x = reinterpret_cast<uintptr_t>(r.args.data), g = reinterpret_cast<uintptr_t>(dlogits);
-  if (g < x + span(r.args.stride) && x < g + span(stride))
+  // Below 2^64 bytes at the largest sizes accepted; the end of either might pass the last address.
+  const auto span = [&](int64_t s) {
+    return ((uint64_t)(r.args.rows - 1) * (uint64_t)s + (uint64_t)r.args.vocab) * (uint64_t)r.bytes;
+  };
+  const uint64_t x = reinterpret_cast<uintptr_t>(r.args.data), g = reinterpret_cast<uintptr_t>(dlogits);
+  if (g > x ? g - x < span(r.args.stride) : x - g < span(stride))
     return fail(RP_ERR_INVALID_ARG, "dlogits overlaps the logits without being them");
   return RP_OK;
 }
