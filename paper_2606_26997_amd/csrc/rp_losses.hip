@@ -107,7 +107,7 @@ __device__ inline void join(const Stats& a, float max, float c, double& s, doubl
 template <int W>
 struct Slots {
   float m[W][3];
-  double d[W][5];
+  double d[W][5], far;
   float out[3];
 };
 template <int W, int N>
@@ -544,12 +544,17 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
     for (int k = 0; k < E; ++k) x[k] = hit >> k & 1 ? -INFINITY : x[k];
   }, slots, so_t, tops);
   const float m = fmaxf(m_o, tops[1]), tm = tops[2];
+  // Entry K stands for what is outside: its largest e.
   // So, and over the list: e, P, and the loss's terms but for ln S:
   // P (ln P - z) with P = exp(t) / total, or e (z - ln P).
   double sums[4] = {so_t[0], 0.0, 0.0, 0.0};
-  for (int j = tid; j < K; j += NT) {
-    if (list[j].id < 0) continue;
-    const double z = ((double)list[j].x - (double)m) * a.inv_t, e = exp(z);
+  for (int j = tid; j <= K; j += NT) {
+    if (j < K && list[j].id < 0) continue;
+    const double z = ((double)(j < K ? list[j].x : m_o) - (double)m) * a.inv_t, e = exp(z);
+    if (j == K) {
+      slots.far = e;
+      continue;
+    }
     const double t = a.kind == RP_DISTILL_TOPK ? (list[j].t - (double)tm) * a.inv_t : list[j].t;
     const double P = exp(t);
     list[j].e = e;
@@ -561,17 +566,20 @@ __global__ __launch_bounds__(threads_of<W>()) void distill_kernel(const DistillA
     else sums[3] += P == 0.0 ? 0.0 : P * (t - z);
   }
   team_sum<W>(sums, slots);
-  const double So = sums[0], far = ((double)m_o - (double)m) * a.inv_t, so = So * exp(far), s = so + sums[1];
-  const double P_sum = sums[2];
+  const double So = sums[0], so = So * slots.far, s = so + sums[1], P_sum = sums[2];
   const bool empty = s == 0.0;
   const bool outside = !(So == 0.0);  // a NaN stays
-  const double ln_s = log(s), qo = so / s, per = (double)w * a.inv_t;
+  const double qo = so / s, per = (double)w * a.inv_t;
   const double left = 1.0 - P_sum, rest = left < 0x1p-24 ? 0x1p-24 : left;  // a NaN stays here too
-  const double gap = log(So) + far - ln_s - log(rest);
+  // The first lanes of every wave take a logarithm each.
+  const int lane = tid % 64;
+  const double logs = log(lane == 0 ? s : lane == 1 ? P_sum : lane == 2 ? So : rest);
+  const double ln_s = __shfl(logs, 0), ln_P = __shfl(logs, 1);
+  const double gap = __shfl(logs, 2) + ((double)m_o - (double)m) * a.inv_t - ln_s - __shfl(logs, 3);
   double loss, whole = 1.0, others;  // others: a token outside has e / So of it as its gradient
   if (a.kind == RP_DISTILL_TOPK) {
     const bool lists = !(P_sum == 0.0);  // an empty list teaches nothing
-    loss = lists ? sums[3] / P_sum - log(P_sum) + ln_s : 0.0 * s;
+    loss = lists ? sums[3] / P_sum - ln_P + ln_s : 0.0 * s;
     others = lists ? qo : 0.0;
   } else if (a.kind == RP_DISTILL_TAIL) {
     loss = sums[3] + P_sum * ln_s - (outside ? rest * gap : 0.0);
