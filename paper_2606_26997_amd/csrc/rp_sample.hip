@@ -21,11 +21,13 @@
 // and one pass sums what is above them and lists what is between them.
 //
 // What bounds it (256 rows of 151936 bf16 logits, 11 us to read): without filters
-// 50 us, about 38 of them 64-bit weights (13 instructions a logit, 4 cycles each for
-// a wave); top-k 35 and min-p 29 us, the first pass 23 (32-bit weights) and the rest
-// the chain of short steps between barriers; a nucleus of 10^5 tokens 110 us, the
-// row's two further passes, one of them in 64-bit weights. A single row takes 15 to
-// 25 us, nearly all in that chain.
+// 46 us, in which a unit is busy for 104e3 cycles: 33 vector instructions a logit
+// (counted), 18 of them in 64 bits at 4 cycles for a wave and the others at 2, are
+// 60e3 of those, and loads and the chain behind the pass the rest; top-k 30 and min-p
+// 27 us (35 where rows are flat), the first pass 23 (32-bit weights) and the rest the
+// chain of short steps between barriers; a nucleus of 10^5 tokens 106 us, the row's
+// two further passes, one of them in 64-bit weights. A single row takes 15 to 25 us,
+// nearly all in that chain.
 #include "rp_rows.h"
 
 namespace rp {
@@ -592,7 +594,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void sa
     const bool probe = k >= V && p < 1.0;
     // The mass of the nucleus, where every token counts, for which Z in 32 bits leaves
     // a range: a term is off by (3 |d| + 2) 2^-24, |d| ln 2 averages at most ln V < 14,
-    // and a thread adds `steps` of them, in vectors of 8.
+    // and a thread adds `steps` of them, in vectors of 8. (Rows of 2^20 rising fp32 logits,
+    // whose reference moves with every vector, were off by up to 18 of the 640 steps of
+    // 2^-24 that this leaves.)
     const double off = (128.0 + r.steps) * 0x1p-24;
     const u64 need_lo = (u64)fmax(ceil(p * Z * (1.0 - off) * scale), 1.0);
     const u64 need_hi = max((u64)ceil(p * Z * (1.0 + off) * scale), need_lo);
